@@ -415,6 +415,47 @@ int coopt_paged_gqa_prefill_chunk_ws(const void* q, const void* k_cache, const v
                                      void* hip_stream);
 
 /*
+ * Attention through a sliding window with the first tokens visible, for models whose layers look back a
+ * bounded distance and keep a sequence's first tokens in sight ("sinks").  A query at position p (counted
+ * from 0) sees the tokens j <= p with j > p - window -- the last `window` tokens, itself included -- or
+ * j < num_sinks; over these it is Eq. 1 with the grouping of Eq. 7, as in the calls without a window:
+ *   out = softmax_j( softmax_scale * q . k~[j] ) . v~[j].
+ * A window of max_blocks_per_seq * 16 tokens or more hides nothing.  A launch reads what its rows see, to whole
+ * blocks: the blocks behind every row's window, but for the first num_sinks tokens', are not read, nor
+ * are their table entries (coopt_kv_blocks_free_outside_window gives them back to the pool and leaves -1 there).
+ * Tokens that no row of a launch sees may hold anything; hidden scores never reach a result.
+ *   window >= 1, num_sinks >= 0; COOPT_ERR_SHAPE otherwise
+ *
+ * Decode: one new token per sequence, at position context_lens[s] - 1.  Arguments as in
+ * coopt_paged_gqa_decode; zeros where context_lens[s] == 0.
+ *   workspace  coopt_decode_window_workspace_bytes(shape, window, num_sinks) bytes, 16-byte aligned, contents
+ *              undefined before and after; NULL where that is 0.  Calls that share it must be ordered.
+ *              It does not grow with the context, only with the window.
+ */
+size_t coopt_decode_window_workspace_bytes(const coopt_shape* shape, int32_t window, int32_t num_sinks);
+int coopt_paged_gqa_decode_window(const void* q, const void* k_cache, const void* v_cache,
+                                  const float* k_scale, const float* v_scale,
+                                  const int32_t* block_tables, const int32_t* context_lens,
+                                  int32_t window, int32_t num_sinks, void* out, void* workspace,
+                                  size_t workspace_bytes, const coopt_shape* shape, void* hip_stream);
+
+/*
+ * Chunked prefill through the window: local row i of sequence s is at position context_lens[s] - C_s + i.
+ * Arguments as in coopt_paged_gqa_prefill_chunk_ws.
+ *   workspace  coopt_prefill_window_workspace_bytes(shape, max_chunk_len, window, num_sinks) bytes, 16-byte
+ *              aligned; NULL where that is 0
+ */
+size_t coopt_prefill_window_workspace_bytes(const coopt_shape* shape, int32_t max_chunk_len, int32_t window,
+                                            int32_t num_sinks);
+int coopt_paged_gqa_prefill_chunk_window(const void* q, const void* k_cache, const void* v_cache,
+                                         const float* k_scale, const float* v_scale,
+                                         const int32_t* block_tables, const int32_t* context_lens,
+                                         const int32_t* query_start, int32_t num_query_rows,
+                                         int32_t max_chunk_len, int32_t window, int32_t num_sinks, void* out,
+                                         void* workspace, size_t workspace_bytes, const coopt_shape* shape,
+                                         void* hip_stream);
+
+/*
  * Dequantising gather (the read half of Opt-KV, Eq. 6; the paper's gather_cached_kv): contiguous
  * fp16 K and V of logical tokens [tok_begin, tok_end) of sequence `seq`:
  *   k_out, v_out [tok_end - tok_begin][H_k][d] fp16, value = fp16(code * scale) (round to nearest

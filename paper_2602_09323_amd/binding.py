@@ -37,6 +37,8 @@ EXPORTS = [
     "coopt_paged_gqa_decode_scheduled", "coopt_status_string",
     "coopt_paged_gqa_decode_noalloc", "coopt_decode_builtin_workspace_bytes",
     "coopt_paged_gqa_prefill_chunk_ws", "coopt_prefill_workspace_bytes",
+    "coopt_paged_gqa_decode_window", "coopt_decode_window_workspace_bytes",
+    "coopt_paged_gqa_prefill_chunk_window", "coopt_prefill_window_workspace_bytes",
 ]
 
 
@@ -98,6 +100,13 @@ def load_library():
                                                          shp, vp]
         lib.coopt_prefill_workspace_bytes.argtypes = [shp, i32]
         lib.coopt_prefill_workspace_bytes.restype = sz
+        lib.coopt_paged_gqa_decode_window.argtypes = [vp, vp, vp, vp, vp, vp, vp, i32, i32, vp, vp, sz, shp, vp]
+        lib.coopt_decode_window_workspace_bytes.argtypes = [shp, i32, i32]
+        lib.coopt_decode_window_workspace_bytes.restype = sz
+        lib.coopt_paged_gqa_prefill_chunk_window.argtypes = [vp, vp, vp, vp, vp, vp, vp, vp, i32, i32, i32, i32, vp, vp, sz,
+                                                             shp, vp]
+        lib.coopt_prefill_window_workspace_bytes.argtypes = [shp, i32, i32, i32]
+        lib.coopt_prefill_window_workspace_bytes.restype = sz
         lib.coopt_gather_cached_kv.argtypes = [vp, vp, vp, vp, vp, i32, i32, i32, vp, vp, shp, vp]
         lib.coopt_decode_schedule_bytes.argtypes = [shp, plp]
         lib.coopt_decode_schedule_bytes.restype = sz
@@ -111,8 +120,8 @@ def load_library():
         lib.coopt_status_string.restype = ctypes.c_char_p
         for name in EXPORTS:
             if name not in ("coopt_decode_workspace_bytes", "coopt_decode_schedule_bytes",
-                            "coopt_prefill_workspace_bytes",
-                            "coopt_status_string", "coopt_default_decode_plan",
+                            "coopt_prefill_workspace_bytes", "coopt_decode_window_workspace_bytes",
+                            "coopt_prefill_window_workspace_bytes", "coopt_status_string", "coopt_default_decode_plan",
                             "coopt_decode_builtin_workspace_bytes"):
                 getattr(lib, name).restype = ctypes.c_int
         _lib = lib
@@ -527,6 +536,57 @@ def paged_gqa_prefill_chunk_ws(q, k_cache, v_cache, k_scale, v_scale, block_tabl
           int(num_query_rows), int(max_chunk_len),
           _dev(out, "out", what, elem=2, min_bytes=rows_bytes), pws, nws, ctypes.byref(shape),
           _stream(stream))
+
+
+# ---------------------------------------------------------------- attention through a sliding window
+
+def _sized_workspace(workspace, need: int, what: str):
+    """A caller's workspace of at least ``need`` bytes; None where none is needed."""
+    if workspace is None and need == 0:
+        return None, 0
+    return _dev(workspace, "workspace", what, need), _nbytes(workspace)
+
+
+def decode_window_workspace_bytes(shape: Shape, window: int, num_sinks: int) -> int:
+    return int(load_library().coopt_decode_window_workspace_bytes(ctypes.byref(shape), int(window), int(num_sinks)))
+
+
+def paged_gqa_decode_window(q, k_cache, v_cache, k_scale, v_scale, block_tables, context_lens, window: int,
+                            num_sinks: int, out, workspace, shape: Shape, stream=None) -> None:
+    """One new token per sequence attends to its last ``window`` tokens and the first ``num_sinks``.
+    workspace: a device buffer of at least decode_window_workspace_bytes(...) bytes (None where that is 0)."""
+    what = "paged_gqa_decode_window"
+    z = _sizes(shape)
+    ins = _decode_inputs(q, k_cache, v_cache, k_scale, v_scale, block_tables, context_lens, z, what)
+    pws, nws = _sized_workspace(workspace, decode_window_workspace_bytes(shape, window, num_sinks), what)
+    _call("coopt_paged_gqa_decode_window",
+          *ins, int(window), int(num_sinks), _dev(out, "out", what, elem=2, min_bytes=z["q"]), pws, nws,
+          ctypes.byref(shape), _stream(stream))
+
+
+def prefill_window_workspace_bytes(shape: Shape, max_chunk_len: int, window: int, num_sinks: int) -> int:
+    return int(load_library().coopt_prefill_window_workspace_bytes(ctypes.byref(shape), int(max_chunk_len),
+                                                                   int(window), int(num_sinks)))
+
+
+def paged_gqa_prefill_chunk_window(q, k_cache, v_cache, k_scale, v_scale, block_tables, context_lens,
+                                   query_start, num_query_rows: int, max_chunk_len: int, window: int,
+                                   num_sinks: int, out, workspace, shape: Shape, stream=None) -> None:
+    """Every row of the chunks through its own window.  workspace: at least prefill_window_workspace_bytes(...)
+    bytes (None where that is 0)."""
+    what = "paged_gqa_prefill_chunk_window"
+    z = _sizes(shape)
+    rows_bytes = int(num_query_rows) * shape.num_q_heads * shape.head_dim * 2
+    need = prefill_window_workspace_bytes(shape, max_chunk_len, window, num_sinks)
+    pws, nws = _sized_workspace(workspace, need, what)
+    _call("coopt_paged_gqa_prefill_chunk_window",
+          _dev(q, "q", what, elem=2, min_bytes=rows_bytes),
+          *_cache_ptrs(k_cache, v_cache, k_scale, v_scale, z),
+          _dev(block_tables, "block_tables", what, dtype=_i32(), min_bytes=z["tables"]),
+          _dev(context_lens, "context_lens", what, dtype=_i32(), min_bytes=z["lens"]),
+          _dev(query_start, "query_start", what, dtype=_i32(), min_bytes=z["lens"] + 4),
+          int(num_query_rows), int(max_chunk_len), int(window), int(num_sinks),
+          _dev(out, "out", what, elem=2, min_bytes=rows_bytes), pws, nws, ctypes.byref(shape), _stream(stream))
 
 
 def decode_schedule_bytes(shape: Shape, plan: Optional[DecodePlan] = None) -> int:

@@ -268,6 +268,37 @@ __device__ __forceinline__ void token_masks(int cache_valid, uint32_t& m0, uint3
     }
 }
 
+// Tokens in front of a column's window (window.hpp), by their distance from the lane's first token of
+// block A (its four of block B are 16 .. 19): [lo, hi) hidden from the lane's column, [lo, hi_all) from
+// every column.  any (wave-uniform): some column has one in this group.
+struct Hole {
+    bool any;
+    int lo, hi, hi_all;
+};
+
+// Zeros V and v_scale of those of the lane's 4 tokens of a block that lie in [lo, hi): whatever they hold
+// meets a weight of zero.
+template <int HEAD_DIM, int KV>
+__device__ __forceinline__ void hide_tokens(BlockRegs<HEAD_DIM, KV>& R, int lo, int hi)
+{
+    uint32_t m0 = 0xffffffffu, m1 = 0xffffffffu;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const bool hidden = i >= lo && i < hi;
+        if constexpr (kIsFp8<KV>) {
+            m0 &= hidden ? ~(0xffu << (8 * i)) : 0xffffffffu;
+            R.vs[i] = hidden ? 0.0f : R.vs[i];
+        } else {
+            (i < 2 ? m0 : m1) &= hidden ? ~(0xffffu << (16 * (i & 1))) : 0xffffffffu;
+        }
+    }
+#pragma unroll
+    for (int j = 0; j < BlockRegs<HEAD_DIM, KV>::NL; ++j) {
+        if constexpr (kIsFp8<KV>) R.v[j] &= m0;
+        else R.v[j] &= u32x4{m0, m1, m0, m1};
+    }
+}
+
 // The group's 2 x 4 scores of this lane in log2 units, z[i] for block A's tokens 4grp+i and
 // z[4+i] for block B's (Opt-KV Eq. 6 dequantisation folded into one multiply per token, Opt-GQA
 // Eq. 8's scaled dot products on the matrix cores), with the tail fix-ups applied.
@@ -280,11 +311,12 @@ __device__ __forceinline__ void token_masks(int cache_valid, uint32_t& m0, uint3
 //                 v_scale of absent tokens are zeroed in place, so stale NaN codes or scales
 //                 cannot reach the accumulators.  The fix-ups sit in small branches that touch only
 //                 temporaries and the loaded tile, so the accumulators stay in place across the loop.
-template <int HEAD_DIM, int KV>
+//   HOLES: besides, `hole` hides some of the tokens in front.
+template <int HEAD_DIM, int KV, bool HOLES = false>
 __device__ __forceinline__ void group_scores(BlockRegs<HEAD_DIM, KV>& A, BlockRegs<HEAD_DIM, KV>& B,
                                              const half8_t (&qop)[HEAD_DIM / 32], bool tail, int visA,
                                              int visB, int cacheA, int cacheB, float scale_log2e,
-                                             float (&z)[8])
+                                             float (&z)[8], const Hole& hole = Hole{})
 {
     floatx4 sA = {0.f, 0.f, 0.f, 0.f}, sB = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
@@ -326,6 +358,17 @@ __device__ __forceinline__ void group_scores(BlockRegs<HEAD_DIM, KV>& A, BlockRe
             } else {
                 A.v[j] &= u32x4{a0, a1, a0, a1};
                 B.v[j] &= u32x4{b0, b1, b0, b1};
+            }
+        }
+    }
+    if constexpr (HOLES) {
+        if (hole.any) {
+            hide_tokens<HEAD_DIM, KV>(A, hole.lo, hole.hi_all);
+            hide_tokens<HEAD_DIM, KV>(B, hole.lo - kBlock, hole.hi_all - kBlock);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                z[i] = fminf(z[i], (i >= hole.lo && i < hole.hi) ? -INFINITY : INFINITY);
+                z[4 + i] = fminf(z[4 + i], (i + kBlock >= hole.lo && i + kBlock < hole.hi) ? -INFINITY : INFINITY);
             }
         }
     }
@@ -386,14 +429,15 @@ __device__ __forceinline__ void group_pv(const BlockRegs<HEAD_DIM, KV>& A,
 //      identical in the four lanes (n, 0..3).
 //   l: this lane's share of the running sum, acc[c][r] = O^T[16c + 4grp + r][n], both times 2^kPShiftOf<KV>.
 // Requirement: whenever m is still -inf, the group holds a token visible to column n.
-template <int HEAD_DIM, int KV>
+template <int HEAD_DIM, int KV, bool HOLES = false>
 __device__ __forceinline__ void group_update(BlockRegs<HEAD_DIM, KV>& A, BlockRegs<HEAD_DIM, KV>& B,
                                              const half8_t (&qop)[HEAD_DIM / 32], float& m, float& l,
                                              floatx4 (&acc)[HEAD_DIM / 16], bool tail, int visA,
-                                             int visB, int cacheA, int cacheB, float scale_log2e)
+                                             int visB, int cacheA, int cacheB, float scale_log2e,
+                                             const Hole& hole = Hole{})
 {
     float z[8];
-    group_scores<HEAD_DIM, KV>(A, B, qop, tail, visA, visB, cacheA, cacheB, scale_log2e, z);
+    group_scores<HEAD_DIM, KV, HOLES>(A, B, qop, tail, visA, visB, cacheA, cacheB, scale_log2e, z, hole);
     const float bm = fmaxf(fmaxf(fmaxf(z[0], z[1]), fmaxf(z[2], z[3])),
                            fmaxf(fmaxf(z[4], z[5]), fmaxf(z[6], z[7])));
     if (__builtin_amdgcn_ballot_w64(bm > m + kRescaleSlack) != 0) {   // wave-uniform, rare
