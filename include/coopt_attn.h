@@ -440,6 +440,19 @@ int coopt_paged_gqa_decode_window(const void* q, const void* k_cache, const void
                                   size_t workspace_bytes, const coopt_shape* shape, void* hip_stream);
 
 /*
+ * The fused step through the window: coopt_kv_cache_write_* of one new token per sequence and the decode above in
+ * one call, as coopt_paged_gqa_decode_step is for the calls without a window (its k, v, slot_mapping and rules).
+ * Where the workspace is of 0 bytes this is one launch, in which the new rows are stored beside the reads of
+ * other sequences.
+ */
+int coopt_paged_gqa_decode_window_step(const void* k, const void* v, const int64_t* slot_mapping,
+                                       const void* q, void* k_cache, void* v_cache, float* k_scale,
+                                       float* v_scale, const int32_t* block_tables,
+                                       const int32_t* context_lens, int32_t window, int32_t num_sinks,
+                                       void* out, void* workspace, size_t workspace_bytes,
+                                       const coopt_shape* shape, void* hip_stream);
+
+/*
  * Chunked prefill through the window: local row i of sequence s is at position context_lens[s] - C_s + i.
  * Arguments as in coopt_paged_gqa_prefill_chunk_ws.
  *   workspace  coopt_prefill_window_workspace_bytes(shape, max_chunk_len, window, num_sinks) bytes, 16-byte

@@ -12,5 +12,5 @@ from .binding import (  # noqa: F401
     make_decode_plan, paged_gqa_decode, paged_gqa_decode_merge, paged_gqa_decode_noalloc, paged_gqa_decode_partitioned,
     paged_gqa_decode_scheduled, paged_gqa_decode_split, paged_gqa_decode_step,
     paged_gqa_prefill_chunk, paged_gqa_prefill_chunk_ws, paged_gqa_reduce, prefill_workspace_bytes,
-    decode_window_workspace_bytes, paged_gqa_decode_window, paged_gqa_prefill_chunk_window, prefill_window_workspace_bytes,
+    decode_window_workspace_bytes, paged_gqa_decode_window, paged_gqa_decode_window_step, paged_gqa_prefill_chunk_window, prefill_window_workspace_bytes,
     status_string)

@@ -37,7 +37,7 @@ EXPORTS = [
     "coopt_paged_gqa_decode_scheduled", "coopt_status_string",
     "coopt_paged_gqa_decode_noalloc", "coopt_decode_builtin_workspace_bytes",
     "coopt_paged_gqa_prefill_chunk_ws", "coopt_prefill_workspace_bytes",
-    "coopt_paged_gqa_decode_window", "coopt_decode_window_workspace_bytes",
+    "coopt_paged_gqa_decode_window", "coopt_decode_window_workspace_bytes", "coopt_paged_gqa_decode_window_step",
     "coopt_paged_gqa_prefill_chunk_window", "coopt_prefill_window_workspace_bytes",
 ]
 
@@ -101,6 +101,8 @@ def load_library():
         lib.coopt_prefill_workspace_bytes.argtypes = [shp, i32]
         lib.coopt_prefill_workspace_bytes.restype = sz
         lib.coopt_paged_gqa_decode_window.argtypes = [vp, vp, vp, vp, vp, vp, vp, i32, i32, vp, vp, sz, shp, vp]
+        lib.coopt_paged_gqa_decode_window_step.argtypes = [vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, i32, i32, vp, vp, sz,
+                                                           shp, vp]
         lib.coopt_decode_window_workspace_bytes.argtypes = [shp, i32, i32]
         lib.coopt_decode_window_workspace_bytes.restype = sz
         lib.coopt_paged_gqa_prefill_chunk_window.argtypes = [vp, vp, vp, vp, vp, vp, vp, vp, i32, i32, i32, i32, vp, vp, sz,
@@ -561,6 +563,22 @@ def paged_gqa_decode_window(q, k_cache, v_cache, k_scale, v_scale, block_tables,
     pws, nws = _sized_workspace(workspace, decode_window_workspace_bytes(shape, window, num_sinks), what)
     _call("coopt_paged_gqa_decode_window",
           *ins, int(window), int(num_sinks), _dev(out, "out", what, elem=2, min_bytes=z["q"]), pws, nws,
+          ctypes.byref(shape), _stream(stream))
+
+
+def paged_gqa_decode_window_step(k, v, slot_mapping, q, k_cache, v_cache, k_scale, v_scale, block_tables,
+                                 context_lens, window: int, num_sinks: int, out, workspace, shape: Shape,
+                                 stream=None) -> None:
+    """The write of one new token per sequence and paged_gqa_decode_window in one call."""
+    what = "paged_gqa_decode_window_step"
+    z = _sizes(shape)
+    pk, pv, ps, T = _new_rows(k, v, slot_mapping, z, what)
+    if T < shape.num_seqs:
+        raise CooptError(f"{what}: slot_mapping has {T} entries, the batch {shape.num_seqs} sequences")
+    ins = _decode_inputs(q, k_cache, v_cache, k_scale, v_scale, block_tables, context_lens, z, what)
+    pws, nws = _sized_workspace(workspace, decode_window_workspace_bytes(shape, window, num_sinks), what)
+    _call("coopt_paged_gqa_decode_window_step",
+          pk, pv, ps, *ins, int(window), int(num_sinks), _dev(out, "out", what, elem=2, min_bytes=z["q"]), pws, nws,
           ctypes.byref(shape), _stream(stream))
 
 

@@ -571,6 +571,64 @@ extern "C" int coopt_paged_gqa_decode_step(const void* k, const void* v,
                          flat_plan(plan), given != nullptr, stream, &append, &cache);
 }
 
+// ---- through a sliding window (window.hpp)
+
+extern "C" size_t coopt_decode_window_workspace_bytes(const coopt_shape* sh, int32_t window, int32_t num_sinks)
+{
+    coopt_decode_plan plan;
+    if (check_shape(sh) != COOPT_OK || check_window(window, num_sinks) != COOPT_OK) return 0;
+    coopt_default_decode_plan(&plan);
+    return window_decode_workspace_bytes(sh, window_of(sh, window, num_sinks), flat_plan(plan));
+}
+
+static int window_decode(const void* q, void* k_cache, void* v_cache, float* k_scale, float* v_scale,
+                         const int32_t* block_tables, const int32_t* context_lens, int32_t window, int32_t num_sinks,
+                         void* out, void* workspace, size_t workspace_bytes, const coopt_shape* sh, void* hip_stream,
+                         const FlatAppend* append)
+{
+    int st = check_shape(sh);
+    if (st != COOPT_OK) return st;
+    st = check_window(window, num_sinks);
+    if (st != COOPT_OK) return st;
+    if (sh->num_seqs == 0) return COOPT_OK;
+    st = check_decode_ptrs(q, k_cache, v_cache, k_scale, v_scale, block_tables, context_lens, sh);
+    if (st != COOPT_OK) return st;
+    if (!out || (append && (!append->k || !append->v || !append->slot_mapping))) return COOPT_ERR_NULL;
+    coopt_decode_plan plan;
+    coopt_default_decode_plan(&plan);
+    const Window w = window_of(sh, window, num_sinks);
+    const size_t need = window_decode_workspace_bytes(sh, w, flat_plan(plan));
+    if (need > 0) {
+        if (!workspace) return COOPT_ERR_NULL;
+        if (workspace_bytes < need || ((uintptr_t)workspace & 15u) != 0) return COOPT_ERR_WORKSPACE;
+    }
+    const FlatCacheW cache{k_cache, v_cache, k_scale, v_scale};
+    return launch_window_decode(q, k_cache, v_cache, k_scale, v_scale, block_tables, context_lens, w, out,
+                                need > 0 ? workspace : nullptr, sh, flat_plan(plan), (hipStream_t)hip_stream, append, &cache);
+}
+
+extern "C" int coopt_paged_gqa_decode_window(const void* q, const void* k_cache, const void* v_cache, const float* k_scale,
+                                             const float* v_scale, const int32_t* block_tables, const int32_t* context_lens,
+                                             int32_t window, int32_t num_sinks, void* out, void* workspace,
+                                             size_t workspace_bytes, const coopt_shape* sh, void* hip_stream)
+{
+    // (written to only by the step below)
+    return window_decode(q, const_cast<void*>(k_cache), const_cast<void*>(v_cache), const_cast<float*>(k_scale),
+                         const_cast<float*>(v_scale), block_tables, context_lens, window, num_sinks, out, workspace,
+                         workspace_bytes, sh, hip_stream, nullptr);
+}
+
+extern "C" int coopt_paged_gqa_decode_window_step(const void* k, const void* v, const int64_t* slot_mapping, const void* q,
+                                                  void* k_cache, void* v_cache, float* k_scale, float* v_scale,
+                                                  const int32_t* block_tables, const int32_t* context_lens, int32_t window,
+                                                  int32_t num_sinks, void* out, void* workspace, size_t workspace_bytes,
+                                                  const coopt_shape* sh, void* hip_stream)
+{
+    const FlatAppend append{k, v, slot_mapping};
+    return window_decode(q, k_cache, v_cache, k_scale, v_scale, block_tables, context_lens, window, num_sinks, out, workspace,
+                         workspace_bytes, sh, hip_stream, &append);
+}
+
 extern "C" size_t coopt_decode_schedule_bytes(const coopt_shape* sh, const coopt_decode_plan* given)
 {
     coopt_decode_plan plan;

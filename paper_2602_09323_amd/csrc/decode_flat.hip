@@ -24,6 +24,7 @@
 #include "attn_tile.hpp"
 #include "decode_internal.hpp"
 #include "kv_quant.hpp"
+#include "window.hpp"
 
 namespace coopt {
 
@@ -55,17 +56,25 @@ __device__ __forceinline__ float wave_sum(float a)
 // every (sequence, KV head) pair `extra` units in front of its groups, the price (in group times)
 // of ending a pair inside a share: the masked last group and the hand-over to the next pair.
 // Shares are cut on the cost axis, so a wave that crosses a pair boundary gets fewer groups.
-struct FlatSchedule {
+// WINDOW: a sequence's groups are those of its view through a window; lengths (`t`) are whole ones all the same.
+template <bool WINDOW>
+struct FlatScheduleOf {
     const int32_t* lens;
     const int64_t* new_slots;   // fused step only: slot of the token each sequence appends, or NULL
     int S, H_k, extra, lane;
     // cache of the first 64 sequences (the whole batch when S <= 64)
     int t0, incl0, total0, cincl0, ctotal0;
+    Window window;
 
-    __device__ __forceinline__ int real_weight(int t) const { return H_k * groups_of(t); }
+    __device__ __forceinline__ int groups(int t) const
+    {
+        if constexpr (WINDOW) return groups_of(WindowView(window, t).t);
+        else return groups_of(t);
+    }
+    __device__ __forceinline__ int real_weight(int t) const { return H_k * groups(t); }
     __device__ __forceinline__ int cost_weight(int t) const
     {
-        return t > 0 ? H_k * (groups_of(t) + extra) : 0;
+        return t > 0 ? H_k * (groups(t) + extra) : 0;
     }
 
     // Tokens of sequence s that this launch attends to.  In the fused step that includes the token
@@ -80,10 +89,11 @@ struct FlatSchedule {
         return new_slots != nullptr && t > 0 && new_slots[s] >= 0;
     }
 
-    __device__ __forceinline__ FlatSchedule(const int32_t* context_lens, const int64_t* appended,
-                                            int num_seqs, int kv_heads, int pair_extra, int lane_id)
+    __device__ __forceinline__ FlatScheduleOf(const int32_t* context_lens, const int64_t* appended,
+                                              int num_seqs, int kv_heads, int pair_extra, int lane_id,
+                                              Window through = Window{})
         : lens(context_lens), new_slots(appended), S(num_seqs), H_k(kv_heads), extra(pair_extra),
-          lane(lane_id)
+          lane(lane_id), window(through)
     {
         t0 = lane < S ? cached_len(lane) : 0;
         incl0 = wave_inclusive_scan(real_weight(t0));
@@ -156,13 +166,14 @@ struct FlatSchedule {
     {
         int seq, first, cfirst, t;
         locate<true>(min(v, ctotal - 1), seq, first, cfirst, t);
-        const int ng = groups_of(t);
+        const int ng = groups(t);
         const int r = v - cfirst;                     // v = ctotal lands past the last pair
         const int g = min(r / (ng + extra), H_k);
         const int gi = min(max(r - g * (ng + extra) - extra, 0), ng);
         return first + min(g * ng + gi, H_k * ng);
     }
 };
+using FlatSchedule = FlatScheduleOf<false>;
 
 struct FlatArgs {
     const half_t* q;
@@ -204,6 +215,7 @@ struct FlatArgs {
     uint32_t sched_tag;
     int32_t sched_regions;
     int32_t sched_stride;
+    Window window;        // kernels through a window only
 };
 
 // How the flattened groups are cut into contiguous shares: `nwg` workgroups, the first `r` with
@@ -305,18 +317,23 @@ __device__ __forceinline__ int attention_partials_of(const FlatArgs& a, const Fl
 // LiveSource derives the schedule in the kernel from the context lengths (and reads the block
 // table); PreparedSource reads records that coopt_decode_schedule_prepare left in memory.
 
-// Lane 2j + h of the current chunk describes block h of entry j.
-struct LiveSource {
+// Lane 2j + h of the current chunk describes block h of entry j.  WINDOW: blocks, groups and t are those of the
+// sequence's view (window.hpp).
+template <bool WINDOW>
+struct LiveSourceOf {
+    static constexpr bool kWindow = WINDOW;
     const FlatArgs& a;
-    const FlatSchedule& sched;
+    const FlatScheduleOf<WINDOW>& sched;
     const FlatCut& cut;
     int lane, share, x_begin, x_end;
     int nc = 0;
     int seq_l = 0, cfirst_l = 0, t_l = 0, g_l = 0, gi_l = 0, tile_l = -1;
     unsigned long long last_mask = 0, append_mask = 0;
+    int lo_l = 0, hi_l = 0;                     // WINDOW: hidden tokens
+    unsigned long long hole_mask = 0;           // entries that have some
 
-    __device__ __forceinline__ LiveSource(const FlatArgs& args, const FlatSchedule& s, const FlatCut& c,
-                                          int lane_id, int share_id, int xb, int xe)
+    __device__ __forceinline__ LiveSourceOf(const FlatArgs& args, const FlatScheduleOf<WINDOW>& s, const FlatCut& c,
+                                            int lane_id, int share_id, int xb, int xe)
         : a(args), sched(s), cut(c), lane(lane_id), share(share_id), x_begin(xb), x_end(xe) {}
     __device__ __forceinline__ int size() const { return x_end - x_begin; }
 
@@ -330,9 +347,18 @@ struct LiveSource {
         for (int xs = xc; xs < xc + nc;) {
             int s, first, cfirst, t;
             sched.template locate<false>(xs, s, first, cfirst, t);
-            const int span_end = first + a.H_k * groups_of(t);     // > xs: the owner has groups
+            const int span_end = first + a.H_k * sched.groups(t);     // > xs: the owner has groups
             if (xl >= xs && xl < span_end) { seq_l = s; first_l = first; cfirst_l = cfirst; t_l = t; }
             xs = span_end;
+        }
+        int lead = 0, skip = 0;
+        if constexpr (WINDOW) {
+            const WindowView v(sched.window, t_l);
+            t_l = v.t;
+            lead = v.lead;
+            skip = v.skip;
+            lo_l = v.lo;
+            hi_l = v.hi;
         }
         const int nb_l = (t_l + kBlock - 1) / kBlock;
         const int ng_l = max((nb_l + 1) >> 1, 1);
@@ -341,7 +367,11 @@ struct LiveSource {
         const int b_l = 2 * gi_l + (lane & 1);
         const bool in_chunk = (lane >> 1) < nc;
         tile_l = -1;
-        if (in_chunk && b_l < nb_l) tile_l = a.block_tables[(size_t)seq_l * a.max_blocks + b_l] * a.H_k + g_l;
+        const int at_l = WINDOW && b_l >= lead ? b_l + skip : b_l;
+        if (in_chunk && b_l < nb_l) tile_l = a.block_tables[(size_t)seq_l * a.max_blocks + at_l] * a.H_k + g_l;
+        if constexpr (WINDOW)
+            hole_mask = __builtin_amdgcn_ballot_w64(in_chunk && (lane & 1) == 0 && hi_l > lo_l &&
+                                                    2 * kBlock * gi_l < hi_l && 2 * kBlock * (gi_l + 1) > lo_l);
         // entries that end a segment: last group of their pair, or last group of the share
         last_mask = __builtin_amdgcn_ballot_w64(
             in_chunk && (lane & 1) == 0 && (gi_l == ng_l - 1 || xl == x_end - 1));
@@ -360,6 +390,13 @@ struct LiveSource {
     __device__ __forceinline__ int rem(int e) const
     {
         return __builtin_amdgcn_readlane(t_l, 2 * e) - 2 * kBlock * __builtin_amdgcn_readlane(gi_l, 2 * e);
+    }
+    // what the window hides of the entry, for a lane of group grp
+    __device__ __forceinline__ Hole hole(int e, int grp) const
+    {
+        const int base = 2 * kBlock * __builtin_amdgcn_readlane(gi_l, 2 * e) + 4 * grp;
+        const int hi = __builtin_amdgcn_readlane(hi_l, 2 * e) - base;
+        return Hole{((hole_mask >> (2 * e)) & 1) != 0, __builtin_amdgcn_readlane(lo_l, 2 * e) - base, hi, hi};
     }
     __device__ __forceinline__ bool last(int e) const { return (last_mask >> (2 * e)) & 1; }
     __device__ __forceinline__ bool appends(int e) const { return (append_mask >> (2 * e)) & 1; }
@@ -396,6 +433,7 @@ struct LiveSource {
         return ps;
     }
 };
+using LiveSource = LiveSourceOf<false>;
 
 // A prepared schedule in memory (32-bit words):
 //   [0] layout tag  [1] status (0, or 1 once a launch found the wrong tag)  [2..15] unused
@@ -416,6 +454,7 @@ typedef unsigned int sched_rec_t __attribute__((ext_vector_type(4)));
 // Lane j of the current chunk holds the record of entry j.  The records of the first chunk are
 // loaded by the kernel before it knows the share's size (a region always has room for 32).
 struct PreparedSource {
+    static constexpr bool kWindow = false;
     const FlatArgs& a;
     const uint32_t* region;
     int lane, count;
@@ -682,6 +721,10 @@ __device__ __forceinline__ void stream_share(const FlatArgs& a, Source& src, uns
                         group_update_block_reduce<HEAD_DIM, KV>(
                             regs[u][0], regs[u][1], q_cur, m, l, acc, rem < 2 * kBlock, visA,
                             visA - kBlock, visA, visA - kBlock, a.scale_log2e, red, lane);
+                    else if constexpr (Source::kWindow)
+                        group_update<HEAD_DIM, KV, true>(regs[u][0], regs[u][1], q_cur, m, l, acc,
+                                                         rem < 2 * kBlock, visA, visA - kBlock, visA,
+                                                         visA - kBlock, a.scale_log2e, src.hole(e, grp));
                     else
                         group_update<HEAD_DIM, KV>(regs[u][0], regs[u][1], q_cur, m, l, acc,
                                                    rem < 2 * kBlock, visA, visA - kBlock, visA,
@@ -753,12 +796,12 @@ __device__ __forceinline__ int share_of_workgroup(int wg, int n)
 
 // One wave per workgroup.  The block numbers of up to 32 groups come from one gathered vector load
 // (lane 2j+h = block h of the j-th group), whatever pairs they belong to.
-template <int HEAD_DIM, int KV, int DEPTH, bool BIG, bool BLOCK_REDUCE, bool APPEND>
+template <int HEAD_DIM, int KV, int DEPTH, bool BIG, bool BLOCK_REDUCE, bool APPEND, bool WINDOW = false>
 __global__ void __launch_bounds__(64)
 flat_stream_kernel(const FlatArgs a)
 {
     const int lane = threadIdx.x;
-    const FlatSchedule sched(a.context_lens, a.new_slots, a.num_seqs, a.H_k, a.pair_extra, lane);
+    const FlatScheduleOf<WINDOW> sched(a.context_lens, a.new_slots, a.num_seqs, a.H_k, a.pair_extra, lane, a.window);
     const int ctotal = sched.cost_total();
     const FlatCut cut(max(ctotal, 1), a.decode_wgs, a.min_share);   // shares of the cost axis
     if (blockIdx.x == 0 && lane == 0) a.ws_header[0] = a.ws_tag;
@@ -770,7 +813,7 @@ flat_stream_kernel(const FlatArgs a)
     if (x_begin >= x_end) return;           // a share that lies inside one pair's extra units
 
     extern __shared__ __attribute__((aligned(16))) unsigned char q_stage[];    // see launch_flat_kernel
-    LiveSource src(a, sched, cut, lane, share, x_begin, x_end);
+    LiveSourceOf<WINDOW> src(a, sched, cut, lane, share, x_begin, x_end);
     stream_share<HEAD_DIM, KV, DEPTH, BIG, BLOCK_REDUCE, APPEND>(a, src, q_stage, lane);
 }
 
@@ -1084,7 +1127,8 @@ constexpr long long kPairs = 256;           // a workgroup holds a CU
 // leaves one partial for the merge launch (which then stores the new rows as well).  Against single
 // wavefronts with shares of at least four groups that derive the schedule of the whole batch first: no
 // scans in front of the block numbers, and a quarter of the groups in a row.
-template <int HEAD_DIM, int KV, bool BIG, bool APPEND, bool PARTS>
+// Through a window (WINDOW) the block numbers wait for the length, one round trip more.
+template <int HEAD_DIM, int KV, bool BIG, bool APPEND, bool PARTS, bool WINDOW = false>
 __global__ void __launch_bounds__(64 * (PARTS ? kPartWaves : kPairWaves), PARTS ? 1 : 2)
 pair_decode_kernel(const FlatArgs a)
 {
@@ -1117,7 +1161,8 @@ pair_decode_kernel(const FlatArgs a)
     // group e of this wavefront, of the pair's groups kWaves at a time to its workgroups in turn
     auto group_of = [&](int e) { return (e * parts + part) * kWaves + wave; };
     const int my_block = 2 * group_of(lane >> 1) + (lane & 1);
-    const int ids = my_block < a.max_blocks ? bt[my_block] : 0;
+    int ids = 0;
+    if constexpr (!WINDOW) ids = my_block < a.max_blocks ? bt[my_block] : 0;
     half8_t q[HEAD_DIM / 32];
     load_q_operand_rows<HEAD_DIM, KV>(q, a.q + (size_t)pair * a.G * HEAD_DIM, a.G, true, n, grp);
     uint32_t row_k = 0, row_v = 0;
@@ -1131,7 +1176,14 @@ pair_decode_kernel(const FlatArgs a)
         }
         appends = a.new_slots[seq] >= 0;
     }
-    const int t = a.context_lens[seq];
+    int t = a.context_lens[seq], hole_lo = 0, hole_hi = 0;
+    if constexpr (WINDOW) {
+        const WindowView v(a.window, t);
+        t = v.t;
+        hole_lo = v.lo;
+        hole_hi = v.hi;
+        if (my_block * kBlock < t) ids = bt[v.block(my_block)];
+    }
     const int nb = (t + kBlock - 1) / kBlock, ng = (nb + 1) >> 1;
     const int first = part * kWaves + wave;
     const int count = first < ng ? min((ng - first - 1) / (kWaves * parts) + 1, kPairGroups) : 0;
@@ -1166,8 +1218,13 @@ pair_decode_kernel(const FlatArgs a)
                     if (appends && gi == ng - 1)
                         take_new_token<HEAD_DIM, KV>(regs[u][0], regs[u][1], row_k, row_v, rem - 1, sums[wave], lane);
                 }
-                group_update<HEAD_DIM, KV>(regs[u][0], regs[u][1], q, m, l, acc, rem < 2 * kBlock, vis, vis - kBlock,
-                                           vis, vis - kBlock, a.scale_log2e);
+                Hole hole{};
+                if constexpr (WINDOW) {
+                    const int base = 2 * kBlock * gi, hi = hole_hi - base - 4 * grp;
+                    hole = Hole{hole_hi > hole_lo && base < hole_hi && base + 2 * kBlock > hole_lo, hole_lo - base - 4 * grp, hi, hi};
+                }
+                group_update<HEAD_DIM, KV, WINDOW>(regs[u][0], regs[u][1], q, m, l, acc, rem < 2 * kBlock, vis, vis - kBlock,
+                                                   vis, vis - kBlock, a.scale_log2e, hole);
             }
             __builtin_amdgcn_sched_barrier(0);
             issue(regs[u], e + DEPTH);
@@ -1227,13 +1284,19 @@ pair_decode_kernel(const FlatArgs a)
     }
 }
 
+// staging area of one q operand + one parked partial (o, m, l per lane) + reduction scratch +
+// the fused step's new K and V row
+template <int HEAD_DIM>
+constexpr size_t flat_lds_bytes()
+{
+    return HEAD_DIM / 32 * 1024 + HEAD_DIM / 16 * 1024 + 512 + 512 + 4 * HEAD_DIM;
+}
+
 template <int HEAD_DIM, int KV, bool BIG, int DEPTH, bool BLOCK_REDUCE, bool APPEND>
 static void launch_flat_kernel(const FlatArgs& a, dim3 grid, hipStream_t stream)
 {
     const dim3 block(64);
-    // staging area of one q operand + one parked partial (o, m, l per lane) + reduction scratch +
-    // the fused step's new K and V row
-    const size_t lds = HEAD_DIM / 32 * 1024 + HEAD_DIM / 16 * 1024 + 512 + 512 + 4 * HEAD_DIM;
+    const size_t lds = flat_lds_bytes<HEAD_DIM>();
     if (a.sched)
         hipLaunchKernelGGL((flat_stream_prepared_kernel<HEAD_DIM, KV, DEPTH, BIG, BLOCK_REDUCE, APPEND>),
                            grid, block, lds, stream, a);
@@ -1544,29 +1607,38 @@ static int pair_parts(const coopt_shape* sh, const FlatPlan& plan)
     return std::max(1, std::min({chunks, each, flat_max_slots(sh, plan)}));
 }
 
-template <bool PARTS>
-static int launch_pairs(const FlatArgs& a, const coopt_shape* sh, unsigned wgs, hipStream_t stream)
+// launch(dim, kv, big, append): the shape's kernel, as types.
+template <class F>
+static int launch_for(const FlatArgs& a, const coopt_shape* sh, F launch)
 {
-    const dim3 grid(wgs), block(64 * (PARTS ? kPartWaves : kPairWaves));
     const bool big = !pool_fits_small(sh), append = a.new_slots != nullptr;
-    auto launch = [&](auto dim, auto kv) {
-        constexpr int D = decltype(dim)::value, KV = decltype(kv)::value;
+    auto of_pool = [&](auto dim, auto kv) {
         if (big) {
-            if (append) hipLaunchKernelGGL((pair_decode_kernel<D, KV, true, true, PARTS>), grid, block, 0, stream, a);
-            else hipLaunchKernelGGL((pair_decode_kernel<D, KV, true, false, PARTS>), grid, block, 0, stream, a);
+            if (append) launch(dim, kv, std::true_type{}, std::true_type{});
+            else launch(dim, kv, std::true_type{}, std::false_type{});
         } else {
-            if (append) hipLaunchKernelGGL((pair_decode_kernel<D, KV, false, true, PARTS>), grid, block, 0, stream, a);
-            else hipLaunchKernelGGL((pair_decode_kernel<D, KV, false, false, PARTS>), grid, block, 0, stream, a);
+            if (append) launch(dim, kv, std::false_type{}, std::true_type{});
+            else launch(dim, kv, std::false_type{}, std::false_type{});
         }
     };
     auto of_dim = [&](auto kv) {
-        if (sh->head_dim == 128) launch(std::integral_constant<int, 128>{}, kv);
-        else launch(std::integral_constant<int, 64>{}, kv);
+        if (sh->head_dim == 128) of_pool(std::integral_constant<int, 128>{}, kv);
+        else of_pool(std::integral_constant<int, 64>{}, kv);
     };
     if (sh->kv_dtype == COOPT_KV_E4M3) of_dim(std::integral_constant<int, COOPT_KV_E4M3>{});
     else if (sh->kv_dtype == COOPT_KV_E5M2) of_dim(std::integral_constant<int, COOPT_KV_E5M2>{});
     else of_dim(std::integral_constant<int, COOPT_KV_FP16>{});
     return launch_status();
+}
+
+template <bool PARTS, bool WINDOW = false>
+static int launch_pairs(const FlatArgs& a, const coopt_shape* sh, unsigned wgs, hipStream_t stream)
+{
+    const dim3 grid(wgs), block(64 * (PARTS ? kPartWaves : kPairWaves));
+    return launch_for(a, sh, [&](auto dim, auto kv, auto big, auto append) {
+        hipLaunchKernelGGL((pair_decode_kernel<decltype(dim)::value, decltype(kv)::value, decltype(big)::value,
+                                               decltype(append)::value, PARTS, WINDOW>), grid, block, 0, stream, a);
+    });
 }
 
 int launch_planned_decode(const void* q, const void* k_cache, const void* v_cache, const float* k_scale, const float* v_scale,
@@ -1604,6 +1676,54 @@ int launch_planned_decode(const void* q, const void* k_cache, const void* v_cach
     const int st = launch_pairs<true>(a, sh, pairs * parts, stream);
     if (st != COOPT_OK) return st;
     return launch_flat_merge(context_lens, workspace, out, sh, plan, stream, nullptr, false, append, cache);
+}
+
+// The same choice for what a window leaves of the sequences, under the library's own plan: the table that
+// bounds the work, and the workspace with it, is as wide as a view (window_shape).
+size_t window_decode_workspace_bytes(const coopt_shape* sh, const Window& window, const FlatPlan& plan)
+{
+    const coopt_shape view = window_shape(sh, window);
+    return sh->num_seqs == 0 || pair_decode_fits(&view) ? 0 : flat_workspace_bytes(&view, plan);
+}
+
+int launch_window_decode(const void* q, const void* k_cache, const void* v_cache, const float* k_scale, const float* v_scale,
+                         const int32_t* block_tables, const int32_t* context_lens, const Window& window, void* out,
+                         void* workspace, const coopt_shape* sh, const FlatPlan& plan, hipStream_t stream,
+                         const FlatAppend* append, const FlatCacheW* cache)
+{
+    const coopt_shape view = window_shape(sh, window);
+    if (flat_max_cost(&view) > 0x7fffffffLL) return COOPT_ERR_SHAPE;
+    FlatArgs a = flat_args(&view, plan, workspace);
+    a.q = (const half_t*)q;
+    a.cv = CacheView{(const uint8_t*)k_cache, (const uint8_t*)v_cache, k_scale, v_scale};
+    a.block_tables = block_tables;
+    a.context_lens = context_lens;
+    a.max_blocks = sh->max_blocks_per_seq;
+    a.window = window;
+    a.out = (half_t*)out;
+    a.kv_dtype = sh->kv_dtype;
+    if (append) {
+        a.new_slots = append->slot_mapping;
+        a.k_new = (const half_t*)append->k;
+        a.v_new = (const half_t*)append->v;
+        a.k_cache_w = (uint8_t*)cache->k_cache;
+        a.v_cache_w = (uint8_t*)cache->v_cache;
+        a.k_scale_w = cache->k_scale;
+        a.v_scale_w = cache->v_scale;
+    }
+    const int pairs = sh->num_seqs * sh->num_kv_heads;
+    if (pair_decode_fits(&view))
+        return launch_pairs<false, true>(a, sh, pairs + (append ? (pairs + kPairWaves - 1) / kPairWaves : 0), stream);
+    a.parts = pair_parts(&view, plan);
+    a.decode_wgs = flat_grid_groups(&view, plan);
+    const int st = a.parts > 0 ? launch_pairs<true, true>(a, sh, pairs * a.parts, stream)
+                               : launch_for(a, sh, [&](auto dim, auto kv, auto big, auto append) {
+        constexpr int D = decltype(dim)::value;
+        hipLaunchKernelGGL((flat_stream_kernel<D, decltype(kv)::value, 2, decltype(big)::value, false, decltype(append)::value, true>),
+                           dim3((unsigned)a.decode_wgs), dim3(64), flat_lds_bytes<D>(), stream, a);
+    });
+    if (st != COOPT_OK) return st;
+    return launch_flat_merge(context_lens, workspace, out, &view, plan, stream, nullptr, false, append, cache);
 }
 
 }  // namespace coopt

@@ -5,6 +5,7 @@
 #include <algorithm>
 
 #include "common.hpp"
+#include "window.hpp"
 
 namespace coopt {
 
@@ -68,5 +69,13 @@ int launch_planned_decode(const void* q, const void* k_cache, const void* v_cach
                   const int32_t* block_tables, const int32_t* context_lens, void* out, void* workspace,
                   const coopt_shape* sh, const FlatPlan& plan, bool own_plan, hipStream_t stream,
                   const FlatAppend* append = nullptr, const FlatCacheW* cache = nullptr);
+
+// Decode or fused step through a window, in the form that suits what the window bounds; workspace bytes 0: in
+// one launch, without a workspace.
+size_t window_decode_workspace_bytes(const coopt_shape* sh, const Window& window, const FlatPlan& plan);
+int launch_window_decode(const void* q, const void* k_cache, const void* v_cache, const float* k_scale, const float* v_scale,
+                         const int32_t* block_tables, const int32_t* context_lens, const Window& window, void* out,
+                         void* workspace, const coopt_shape* sh, const FlatPlan& plan, hipStream_t stream,
+                         const FlatAppend* append = nullptr, const FlatCacheW* cache = nullptr);
 
 }  // namespace coopt

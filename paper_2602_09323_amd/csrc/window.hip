@@ -54,32 +54,6 @@ __device__ __forceinline__ void stream_view(const WindowArgs& a, const WindowVie
 
 template <int HEAD_DIM, int KV, bool BIG>
 __global__ void __launch_bounds__(64)
-window_decode_kernel(const WindowArgs a)
-{
-    const int lane = threadIdx.x, n = lane & 15, grp = lane >> 4;
-    const int pair = blockIdx.x, seq = pair / a.H_k, g = pair - seq * a.H_k;
-    const int t = a.context_lens[seq];
-    floatx4 acc[HEAD_DIM / 16];
-    float l = 0.0f;
-#pragma unroll
-    for (int c = 0; c < HEAD_DIM / 16; ++c) acc[c] = floatx4{0.f, 0.f, 0.f, 0.f};
-    if (t > 0) {
-        half8_t q[HEAD_DIM / 32];
-        load_q_operand_rows<HEAD_DIM, KV>(q, a.q + (size_t)pair * a.G * HEAD_DIM, a.G, true, n, grp);
-        const WindowView v(a.window, t);
-        stream_view<HEAD_DIM, KV, BIG>(a, v, seq, g, v.t, v.hi, v.hi, q, acc, l, lane);
-    }
-    if (n >= a.G) return;
-    const float inv = t > 0 ? 1.0f / l : 0.0f;
-    half_t* row = a.out + ((size_t)pair * a.G + n) * HEAD_DIM + 4 * grp;
-#pragma unroll
-    for (int c = 0; c < HEAD_DIM / 16; ++c)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) row[16 * c + i] = (half_t)(acc[c][i] * inv);
-}
-
-template <int HEAD_DIM, int KV, bool BIG>
-__global__ void __launch_bounds__(64)
 window_prefill_kernel(const WindowArgs a)
 {
     const int lane = threadIdx.x, n = lane & 15, grp = lane >> 4;
@@ -107,13 +81,6 @@ window_prefill_kernel(const WindowArgs a)
 }  // namespace coopt
 
 using namespace coopt;
-
-static int check_window(const coopt_shape* sh, int window, int num_sinks)
-{
-    const int st = check_shape(sh);
-    if (st != COOPT_OK) return st;
-    return window >= 1 && num_sinks >= 0 ? COOPT_OK : COOPT_ERR_SHAPE;
-}
 
 static WindowArgs window_args(const void* q, const void* k_cache, const void* v_cache, const float* k_scale, const float* v_scale,
                               const int32_t* block_tables, const int32_t* context_lens, int window, int num_sinks, void* out,
@@ -148,30 +115,9 @@ static void for_cache(const coopt_shape* sh, F launch)
     else of_dim(std::integral_constant<int, COOPT_KV_FP16>{});
 }
 
-extern "C" size_t coopt_decode_window_workspace_bytes(const coopt_shape* sh, int32_t window, int32_t num_sinks) { return 0; }
-
 extern "C" size_t coopt_prefill_window_workspace_bytes(const coopt_shape* sh, int32_t max_chunk_len, int32_t window, int32_t num_sinks)
 {
     return 0;
-}
-
-extern "C" int coopt_paged_gqa_decode_window(const void* q, const void* k_cache, const void* v_cache, const float* k_scale,
-                                             const float* v_scale, const int32_t* block_tables, const int32_t* context_lens,
-                                             int32_t window, int32_t num_sinks, void* out, void* workspace,
-                                             size_t workspace_bytes, const coopt_shape* sh, void* hip_stream)
-{
-    const int st = check_window(sh, window, num_sinks);
-    if (st != COOPT_OK) return st;
-    if (sh->num_seqs == 0) return COOPT_OK;
-    if (!q || !k_cache || !v_cache || !block_tables || !context_lens || !out) return COOPT_ERR_NULL;
-    if (sh->kv_dtype != COOPT_KV_FP16 && (!k_scale || !v_scale)) return COOPT_ERR_NULL;
-    const WindowArgs a = window_args(q, k_cache, v_cache, k_scale, v_scale, block_tables, context_lens, window, num_sinks, out, sh);
-    const dim3 grid((unsigned)((long long)sh->num_seqs * sh->num_kv_heads));
-    for_cache(sh, [&](auto dim, auto kv, auto big) {
-        hipLaunchKernelGGL((window_decode_kernel<decltype(dim)::value, decltype(kv)::value, decltype(big)::value>), grid, dim3(64), 0,
-                           (hipStream_t)hip_stream, a);
-    });
-    return launch_status();
 }
 
 extern "C" int coopt_paged_gqa_prefill_chunk_window(const void* q, const void* k_cache, const void* v_cache, const float* k_scale,
@@ -181,7 +127,9 @@ extern "C" int coopt_paged_gqa_prefill_chunk_window(const void* q, const void* k
                                                     int32_t num_sinks, void* out, void* workspace, size_t workspace_bytes,
                                                     const coopt_shape* sh, void* hip_stream)
 {
-    const int st = check_window(sh, window, num_sinks);
+    int st = check_shape(sh);
+    if (st != COOPT_OK) return st;
+    st = check_window(window, num_sinks);
     if (st != COOPT_OK) return st;
     if (num_query_rows < 0 || max_chunk_len < 0) return COOPT_ERR_SHAPE;
     if (sh->num_seqs == 0 || num_query_rows == 0 || max_chunk_len == 0) return COOPT_OK;

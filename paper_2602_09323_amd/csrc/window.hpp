@@ -43,6 +43,9 @@ struct WindowView {
     __device__ __forceinline__ int block(int b) const { return b < lead ? b : b + skip; }
 };
 
+// Arguments of the entry points; behind check_shape.
+inline int check_window(int window, int num_sinks) { return window >= 1 && num_sinks >= 0 ? COOPT_OK : COOPT_ERR_SHAPE; }
+
 // Both clamped to what a table holds (2^28 tokens at most: no sum overflows).
 inline Window window_of(const coopt_shape* sh, int window, int num_sinks)
 {

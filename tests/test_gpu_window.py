@@ -75,6 +75,54 @@ def test_decode_of_longer_contexts(oracle_mod, kv, H_q, H_k, d, lens, window, si
     assert_close(hip_decode_window(w, cache_to_dev(cache), tables, window, sinks), ref, f"window {window} sinks {sinks}")
 
 
+@pytest.mark.parametrize("lens,window,sinks", [(LENS, 1, 0), (LENS, 17, 4), (LENS, 333, 33), ([2500, 1, 0, 700], 2048, 4),
+                                               ([1200] * 70 + [5] * 3, 512, 4)])
+@pytest.mark.parametrize("kv,H_q,H_k,d", HEADS)
+def test_fused_step(oracle_mod, kv, H_q, H_k, d, lens, window, sinks):
+    """The write of the new tokens and the attention in one call: every third sequence's slot is negative (nothing
+    written, its last token read from the cache).  Cache bytes as the separate write leaves them."""
+    w = random_workload("window_step", 21, kv, H_q, H_k, d, lens)
+    cache, tables = poisoned(oracle_mod, w, hidden_from(w, [1] * w.S, window, sinks))
+    ref = window_attention(w, cache, w.q, w.context_lens, np.arange(w.S + 1), window, sinks)
+    last = np.asarray(w.seq_start[1:]) - 1
+    some = [s for s in range(w.S) if lens[s] > 0 and s % 3 != 2]
+    slots = np.full(w.S, -1, np.int64)
+    slots[some] = w.slots[last[some]]
+    new = np.zeros((2, w.S, H_k, d), np.float16)
+    new[0, some], new[1, some] = w.k_ctx[last[some]], w.v_ctx[last[some]]
+    dcache, shape = cache_to_dev(cache), shape_of(w)
+    before = [None if x is None else x.clone() for x in dcache]
+    for x in dcache:                                   # the rows that the step brings: not there yet
+        if x is not None:
+            y = x.view(torch.uint8).view(w.NB, -1)
+            for s in some:
+                if lens[s] % 16 == 1:                  # the block's first token: the whole block is stale
+                    y[int(slots[s]) // 16] = 0x7F
+    out = torch.full((w.S, H_q, d), -7.0, dtype=torch.float16, device="cuda")
+    ws = workspace_for(coopt.decode_window_workspace_bytes(shape, window, sinks))
+    coopt.paged_gqa_decode_window_step(dev(new[0].view(np.uint16)), dev(new[1].view(np.uint16)), dev(slots), dev(w.q.view(np.uint16)),
+                                       *dcache, dev(tables), dev(w.context_lens), window, sinks, out, ws, shape)
+    torch.cuda.synchronize()
+    assert_close(out.cpu().numpy().astype(np.float64), ref, f"step window {window} sinks {sinks}")
+    # what the separate write leaves, over the same stale bytes
+    want = [None if x is None else x.clone() for x in before]
+    for x in want:
+        if x is not None:
+            y = x.view(torch.uint8).view(w.NB, -1)
+            for s in some:
+                if lens[s] % 16 == 1:
+                    y[int(slots[s]) // 16] = 0x7F
+    rows = dev(new[0].view(np.uint16)), dev(new[1].view(np.uint16)), dev(slots)
+    if kv == "fp16":
+        coopt.kv_cache_write_fp16(*rows, want[0], want[1], shape)
+    else:
+        coopt.kv_cache_write_fp8(*rows, *want, shape)
+    torch.cuda.synchronize()
+    for name, a, b in zip(("k_cache", "v_cache", "k_scale", "v_scale"), dcache, want):
+        if a is not None:
+            assert torch.equal(a.view(torch.uint8), b.view(torch.uint8)), name
+
+
 @pytest.mark.parametrize("window,sinks", WINDOWS)
 @pytest.mark.parametrize("kv,H_q,H_k,d", HEADS)
 def test_prefill(oracle_mod, kv, H_q, H_k, d, window, sinks):

@@ -92,6 +92,12 @@ def test_refusals(lib):  # noqa: F811
         assert call(window=0) == -2 and call(window=-5) == -2 and call(sinks=-1) == -2
         assert call(shape=_shape(head_dim=96)) == -2 and call(shape=_shape(kv_dtype=7)) == -2
         assert call(shape=_shape(num_seqs=0)) == 0
+    step = lib.coopt_paged_gqa_decode_window_step
+    wide = _shape(num_seqs=64, max_blocks_per_seq=2048)
+    need = lib.coopt_decode_window_workspace_bytes(ctypes.byref(wide), 4096, 4)
+    for k, v, slots in ((None, one, one), (one, None, one), (one, one, None)):
+        assert step(k, v, slots, one, one, one, one, one, one, one, 4096, 4, one, one, size(need), ctypes.byref(wide), None) == -1
+    assert step(one, one, one, one, one, one, one, one, one, one, 0, 4, one, one, size(need), ctypes.byref(wide), None) == -2
     assert decode(q=None) == -1 and decode(out=None) == -1 and decode(ks=None) == -1
     assert prefill(qs=None) == -1 and prefill(vs=None) == -1
     assert prefill(rows=-1) == -2 and prefill(longest=-1) == -2 and prefill(rows=0) == 0 and prefill(longest=0) == 0
