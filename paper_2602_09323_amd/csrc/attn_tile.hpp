@@ -276,26 +276,33 @@ struct Hole {
     int lo, hi, hi_all;
 };
 
+// Clears the lane's tokens [lo, hi) (of 4) in the masks of token_masks.
+template <int KV>
+__device__ __forceinline__ void range_masks(int lo, int hi, uint32_t& m0, uint32_t& m1)
+{
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const bool hidden = i >= lo && i < hi;
+        if constexpr (kIsFp8<KV>) m0 &= hidden ? ~(0xffu << (8 * i)) : 0xffffffffu;
+        else (i < 2 ? m0 : m1) &= hidden ? ~(0xffffu << (16 * (i & 1))) : 0xffffffffu;
+    }
+}
+
 // Zeros V and v_scale of those of the lane's 4 tokens of a block that lie in [lo, hi): whatever they hold
 // meets a weight of zero.
 template <int HEAD_DIM, int KV>
 __device__ __forceinline__ void hide_tokens(BlockRegs<HEAD_DIM, KV>& R, int lo, int hi)
 {
     uint32_t m0 = 0xffffffffu, m1 = 0xffffffffu;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const bool hidden = i >= lo && i < hi;
-        if constexpr (kIsFp8<KV>) {
-            m0 &= hidden ? ~(0xffu << (8 * i)) : 0xffffffffu;
-            R.vs[i] = hidden ? 0.0f : R.vs[i];
-        } else {
-            (i < 2 ? m0 : m1) &= hidden ? ~(0xffffu << (16 * (i & 1))) : 0xffffffffu;
-        }
-    }
+    range_masks<KV>(lo, hi, m0, m1);
 #pragma unroll
     for (int j = 0; j < BlockRegs<HEAD_DIM, KV>::NL; ++j) {
         if constexpr (kIsFp8<KV>) R.v[j] &= m0;
         else R.v[j] &= u32x4{m0, m1, m0, m1};
+    }
+    if constexpr (kIsFp8<KV>) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) R.vs[i] = (i >= lo && i < hi) ? 0.0f : R.vs[i];
     }
 }
 

@@ -47,10 +47,13 @@
 // workgroup 6-8 us after the stream's end, so 3), the block numbers of three stages are asked for
 // before anything else, and nothing is read ahead of the stream (a pass over all v_scales for their
 // largest took 3-6 us a workgroup).  Together: the three prompts 102 -> 90 us, 8 x 352 rows 92 -> 80.
+#include <algorithm>
+
 #include "attn_tile.hpp"
 #include "kv_quant.hpp"
 #include "launch_grid.hpp"
 #include "prefill_deal.hpp"
+#include "window.hpp"
 
 namespace coopt {
 
@@ -68,6 +71,7 @@ struct PrefillArgs : PrefillDeal {
     float scale_log2e;
     float* part;              // the split workgroups' partial rows, in the workspace
     int32_t rank_bits;        // > 0: workgroups in the order of their streams' lengths, which have so many bits (in stages)
+    Window window;            // kernels through a window only
 };
 
 constexpr int kPrefillGroupsPerStage = kPrefillStageTokens / (2 * kBlock);      // two-block groups between two barriers
@@ -148,8 +152,22 @@ __device__ __forceinline__ half2_t wide_weights(const floatx16& s, int k, float 
                    (half_t)__builtin_amdgcn_exp2f(__builtin_fmaf(s[k + 1], scale, -mm))};
 }
 
+// ... of which the tokens [lo, hi) are hidden, too.
+__device__ __forceinline__ float wide_logits_window(floatx16& z, int j, floatx4 ksc, floatx4 lv, int vis, int lo, int hi)
+{
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const float x = __builtin_fmaf(z[4 * j + i], ksc[i], lv[i]);
+        z[4 * j + i] = i < vis && !(i >= lo && i < hi) ? x : -INFINITY;
+    }
+    return fmaxf(fmaxf(z[4 * j], z[4 * j + 1]), fmaxf(z[4 * j + 2], z[4 * j + 3]));
+}
+
 // TILES: of a workgroup, 16 or, where a pair has no more, 8 (whose first four waves alone consume).
-template <int HEAD_DIM, int KV, int TILES, bool BIG>
+// WINDOW: a workgroup streams its rows' view of the sequence (window.hpp) from the first row's window on, and
+// tokens, blocks and lengths are that view's.  A column's window begins up to a workgroup's rows behind the
+// stream's start: the stages in front of the last one's window go group by group, like those at the stream's end.
+template <int HEAD_DIM, int KV, int TILES, bool BIG, bool WINDOW = false>
 __global__ void __launch_bounds__(64 * kPrefillWaves, 2)
 prefill_chunk_kernel(const PrefillArgs a)
 {
@@ -166,7 +184,7 @@ prefill_chunk_kernel(const PrefillArgs a)
     const int team = wave_id >> 2;                     // which groups of a stage it produces: below
     const int n = lane & 15, grp = lane >> 4;
     int pair, turn, qs, C, t;
-    if (a.rank_bits > 0) {
+    if (!WINDOW && a.rank_bits > 0) {
         // Lane p: the XCD's p-th pair.  The stream length (in stages) of the workgroup that I am in the
         // order of all pairs' items by length, bit by bit; then which of the items of that length.
         const int my_pair = 8 * lane + (int)(blockIdx.x & 7), rank = blockIdx.x >> 3;
@@ -200,7 +218,7 @@ prefill_chunk_kernel(const PrefillArgs a)
     }
     const int seq = a.kv_heads.quotient(pair);
     const int g = pair - seq * a.H_k;
-    const int t_ctx = t - C;
+    int t_ctx = t - C;
     const int tiles_per_head = (C + 15) / 16;
     const int total_tiles = a.G * tiles_per_head;
     const PrefillShare share = prefill_share(a, turn, t, C, total_tiles);
@@ -216,10 +234,21 @@ prefill_chunk_kernel(const PrefillArgs a)
     const bool active = wave_id * NR < TILES && first < count;     // a wave without tiles still produces
 
     constexpr int NQ = HEAD_DIM / 16;                  // q operands
-    // Lane r works out tile r of the wave, lane NR the workgroup's last, which sees furthest.
+    // Lane r works out tile r of the wave, lane NR the workgroup's last, which sees furthest (lane NR + 1
+    // through a window its first, which sees furthest back).
     int tile_row, tile_head;
     order.at(lane < NR ? min(first + lane, count - 1)             // surplus tiles repeat the last
-                       : min((block + 1) * TILES, count) - 1, tile_row, tile_head);
+                       : WINDOW && lane == NR + 1 ? block * TILES : min((block + 1) * TILES, count) - 1, tile_row, tile_head);
+    int lead = 0, skip = 0, gap_lo = 0, gap_hi = 0;
+    if constexpr (WINDOW) {
+        const WindowView v(a.window, t, t_ctx + 16 * __builtin_amdgcn_readlane(tile_row, NR + 1) + 1 - a.window.size);
+        lead = v.lead;
+        skip = v.skip;
+        gap_lo = v.lo;
+        gap_hi = v.hi;
+        t = v.t;
+        t_ctx -= skip * kBlock;
+    }
     const int wg_max = t_ctx + min(16 * __builtin_amdgcn_readlane(tile_row, NR) + 15, C - 1) + 1;
     const int nblk = (wg_max + kBlock - 1) / kBlock;
     const int num_groups = (nblk + 1) >> 1;
@@ -260,7 +289,8 @@ prefill_chunk_kernel(const PrefillArgs a)
     const __amdgpu_buffer_rsrc_t bt_rsrc = TileLoader<HEAD_DIM, KV, BIG>::rsrc(bt, a.max_blocks * 4);
     auto load_ids = [&](int stage) {
         const int p = stage * GPS + (team == 0 ? 0 : kFirst) + (lane >> 1);
-        const int b = min(2 * p + (lane & 1), nblk - 1);
+        int b = min(2 * p + (lane & 1), nblk - 1);
+        if constexpr (WINDOW) b = b < lead ? b : b + skip;
         return __builtin_amdgcn_raw_buffer_load_b32(bt_rsrc, lane < 2 * kOwn ? 4 * b : 0, 0, 0);
     };
     auto id_of = [&](uint32_t ids, int i, int b) { return __builtin_amdgcn_readlane((int)ids, 2 * i + b); };
@@ -370,7 +400,11 @@ prefill_chunk_kernel(const PrefillArgs a)
                     // entries are taken times a power of two, 1 over the one just above the largest scale so
                     // far, which the group's row sums are multiplied by again: both are exact.
                     const bool there = my_token + (n >= 8 ? kBlock : 0) < t - 32 * p;      // (else a stale scale)
-                    const float vs = there ? psc : 0.0f;
+                    float vs = there ? psc : 0.0f;
+                    if constexpr (WINDOW) {                    // (nor one that no row sees)
+                        const int token = 32 * p + my_token + (n >= 8 ? kBlock : 0);
+                        vs = token >= gap_lo && token < gap_hi ? 0.0f : vs;
+                    }
                     if ((n & 4) == 0) *dst = __builtin_amdgcn_logf(vs);                    // log2; -inf: absent
                     // (kept from group to group: one vote in the place of a reduction, but where a scale is
                     // larger than all before it)
@@ -394,6 +428,13 @@ prefill_chunk_kernel(const PrefillArgs a)
             if (32 * p + 2 * kBlock > t) {          // wave-uniform: only the cache's last group
                 token_masks<KV>(cacheA, a0, a1);
                 token_masks<KV>(cacheB, b0, b1);
+            }
+            if constexpr (WINDOW) {
+                if (32 * p < gap_hi && 32 * p + 2 * kBlock > gap_lo) {     // wave-uniform: what no row sees
+                    const int at = 32 * p + 4 * grp;
+                    range_masks<KV>(gap_lo - at, gap_hi - at, a0, a1);
+                    range_masks<KV>(gap_lo - at - kBlock, gap_hi - at - kBlock, b0, b1);
+                }
             }
 #pragma unroll
             for (int jj = 0; jj < NLH; ++jj) {
@@ -421,6 +462,8 @@ prefill_chunk_kernel(const PrefillArgs a)
 
     // ---- consumer side
     const int full_limit = min(t, t_ctx + min_row + 1);   // tokens visible to every column of mine
+    // (WINDOW: where the windows of my columns begin, the first and the last of them)
+    const int lower_min = full_limit - a.window.size, lower_max = my_max - a.window.size;
     auto op = [&](const unsigned char* st, int at) { return *reinterpret_cast<const half8_t*>(st + at + 16 * lane); };
     auto scales = [&](const unsigned char* st, int at) { return *reinterpret_cast<const floatx4*>(st + St::kS + at); };
     // My row-sum operand: the cut reciprocals and the rest of tokens 8u + 4h .. are rows 0 and 1 in the lanes
@@ -444,7 +487,8 @@ prefill_chunk_kernel(const PrefillArgs a)
     };
     auto consume = [&](const unsigned char* st, int gi) {
         const int baseA = 2 * gi * kBlock;
-        const bool tail = baseA + 2 * kBlock > full_limit;        // (a missing block B is beyond every limit)
+        bool tail = baseA + 2 * kBlock > full_limit;              // (a missing block B is beyond every limit)
+        if constexpr (WINDOW) tail = tail || (baseA < lower_max && baseA + 2 * kBlock > gap_lo);
         floatx16 z = {};
 #pragma unroll
         for (int k = 0; k < NQ; ++k) z = mfma_32x32x16(op(st, St::kK + 1024 * k), qop[k], z);
@@ -456,8 +500,14 @@ prefill_chunk_kernel(const PrefillArgs a)
                 ksc = scales(st, 32 * j + 16 * h);
                 lv = scales(st, 128 + 32 * j + 16 * h);
             }
-            bm = fmaxf(bm, tail ? wide_logits<true>(z, j, ksc, lv, limit - baseA - 8 * j - 4 * h)
-                                : wide_logits<false>(z, j, ksc, lv, 0));
+            if constexpr (WINDOW) {
+                const int vis = limit - baseA - 8 * j - 4 * h;
+                bm = fmaxf(bm, tail ? wide_logits_window(z, j, ksc, lv, vis, gap_lo - baseA - 8 * j - 4 * h, vis - a.window.size)
+                                    : wide_logits<false>(z, j, ksc, lv, 0));
+            } else {
+                bm = fmaxf(bm, tail ? wide_logits<true>(z, j, ksc, lv, limit - baseA - 8 * j - 4 * h)
+                                    : wide_logits<false>(z, j, ksc, lv, 0));
+            }
         }
         raise(bm);
         const float mm = m - kPShift;
@@ -657,6 +707,21 @@ prefill_chunk_kernel(const PrefillArgs a)
     // over at different stages; each passes one barrier per stage.)
     int si = s_lo;
     const int whole_stages = min(active ? min(g_end, full_limit / (2 * kBlock)) / GPS : 0, s_hi);
+    if constexpr (WINDOW) {
+        // in front of the last column's window, unless that begins among the sinks
+        const int head = min(active && lower_max > gap_lo ? (lower_max + kPrefillStageTokens - 1) / kPrefillStageTokens : 0, s_hi);
+#pragma unroll 1
+        for (; si < head; ++si) {
+#pragma unroll 1
+            for (int gi = si * GPS; gi < min((si + 1) * GPS, g_end) && 2 * gi * kBlock < my_max; ++gi)
+                // (not those that only other waves' columns see)
+                if (2 * gi * kBlock < gap_lo || 2 * (gi + 1) * kBlock > lower_min) consume(slot(gi - si * GPS), gi);
+#pragma unroll
+            for (int i = 0; i < kOwn; ++i) produce(si, i);
+            __syncthreads();
+            next_stage();
+        }
+    }
     if (si < whole_stages) {
         pipeline_start();
         for (; si < whole_stages; ++si) {
@@ -696,7 +761,9 @@ prefill_chunk_kernel(const PrefillArgs a)
 #pragma unroll 1
         for (int gi = parts == 1 ? 0 : quotient(stages * part, parts) * GPS; gi < g_end && 2 * gi * kBlock < my_max; ++gi) {
             auto tile_of = [&](int b) {                        // (no read beyond the table or the pool)
-                const int tile = bt[min(min(2 * gi + b + 1, nblk), a.max_blocks) - 1] * a.H_k + g;
+                int at = min(min(2 * gi + b + 1, nblk), a.max_blocks) - 1;
+                if constexpr (WINDOW) at = min(at < lead ? at : at + skip, a.max_blocks - 1);
+                const int tile = bt[at] * a.H_k + g;
                 return (uint32_t)tile < (uint32_t)a.pool_tiles ? tile : 0;
             };
             const uint8_t* row = a.cv.k_cache + (size_t)tile_of((lane >> 4) & 1) * (kBlock * HEAD_DIM * ES) + 16 * n;
@@ -716,13 +783,14 @@ prefill_chunk_kernel(const PrefillArgs a)
             for (int j = 0; j < 4; ++j) {
                 const size_t at = (size_t)tile_of(j >> 1) * kBlock + 8 * (j & 1) + 4 * h;
                 const int vis = limit - 2 * gi * kBlock - 8 * j - 4 * h;
+                const int lo = gap_lo - 2 * gi * kBlock - 8 * j - 4 * h, hi = vis - a.window.size;
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     const float vs = FP8 ? a.cv.v_scale[at + i] : 1.0f;
                     const float x = FP8 ? __builtin_fmaf(z[4 * j + i], a.cv.k_scale[at + i] * scale, __builtin_amdgcn_logf(vs))
                                         : z[4 * j + i] * scale;
                     const float w = (float)(half_t)__builtin_amdgcn_exp2f(x - mm);
-                    again += i < vis ? (vs > 0.0f ? w * __builtin_amdgcn_rcpf(vs) : w * 0.0f) : 0.0f;
+                    again += i < vis && !(WINDOW && i >= lo && i < hi) ? (vs > 0.0f ? w * __builtin_amdgcn_rcpf(vs) : w * 0.0f) : 0.0f;
                 }
             }
         }
@@ -867,7 +935,8 @@ extern "C" size_t coopt_prefill_workspace_bytes(const coopt_shape* sh, int32_t m
 static int prefill_chunk(const void* q, const void* k_cache, const void* v_cache, const float* k_scale,
                          const float* v_scale, const int32_t* block_tables, const int32_t* context_lens,
                          const int32_t* query_start, int32_t num_query_rows, int32_t max_chunk_len,
-                         void* out, void* workspace, const coopt_shape* sh, void* hip_stream);
+                         void* out, void* workspace, const coopt_shape* sh, void* hip_stream,
+                         const Window* window = nullptr);
 
 extern "C" int coopt_paged_gqa_prefill_chunk(const void* q, const void* k_cache, const void* v_cache,
                                              const float* k_scale, const float* v_scale,
@@ -879,6 +948,52 @@ extern "C" int coopt_paged_gqa_prefill_chunk(const void* q, const void* k_cache,
 {
     return prefill_chunk(q, k_cache, v_cache, k_scale, v_scale, block_tables, context_lens, query_start,
                          num_query_rows, max_chunk_len, out, nullptr, sh, hip_stream);
+}
+
+// ---- through a sliding window (window.hpp): the same launches, planned for streams as long as a window and the sinks
+
+// What a row sees at most.
+static long long window_stream_tokens(const coopt_shape* sh, const Window& w)
+{
+    return std::min((long long)sh->max_blocks_per_seq * kBlock, (long long)w.size + w.sinks);
+}
+
+static size_t window_workspace_bytes(const coopt_shape* sh, int max_chunk_len, const Window& w)
+{
+    const PrefillLaunchPlan lp(sh, max_chunk_len, true);
+    PrefillDeal deal{};
+    deal.set(lp, sh->num_seqs * sh->num_kv_heads, window_stream_tokens(sh, w));
+    return deal.split < 2 ? 0 : lp.workspace_bytes(sh);
+}
+
+extern "C" size_t coopt_prefill_window_workspace_bytes(const coopt_shape* sh, int32_t max_chunk_len, int32_t window,
+                                                       int32_t num_sinks)
+{
+    if (check_shape(sh) != COOPT_OK || check_window(window, num_sinks) != COOPT_OK || max_chunk_len <= 0 || sh->num_seqs == 0)
+        return 0;
+    return window_workspace_bytes(sh, max_chunk_len, window_of(sh, window, num_sinks));
+}
+
+extern "C" int coopt_paged_gqa_prefill_chunk_window(const void* q, const void* k_cache, const void* v_cache, const float* k_scale,
+                                                    const float* v_scale, const int32_t* block_tables,
+                                                    const int32_t* context_lens, const int32_t* query_start,
+                                                    int32_t num_query_rows, int32_t max_chunk_len, int32_t window,
+                                                    int32_t num_sinks, void* out, void* workspace, size_t workspace_bytes,
+                                                    const coopt_shape* sh, void* hip_stream)
+{
+    int st = check_shape(sh);
+    if (st != COOPT_OK) return st;
+    st = check_window(window, num_sinks);
+    if (st != COOPT_OK) return st;
+    const Window w = window_of(sh, window, num_sinks);
+    if (max_chunk_len > 0 && num_query_rows > 0 && sh->num_seqs > 0) {
+        const size_t need = window_workspace_bytes(sh, max_chunk_len, w);
+        if (need > 0 && !workspace) return COOPT_ERR_NULL;
+        if (workspace_bytes < need || (need > 0 && ((uintptr_t)workspace & 15u) != 0)) return COOPT_ERR_WORKSPACE;
+        if (need == 0) workspace = nullptr;
+    }
+    return prefill_chunk(q, k_cache, v_cache, k_scale, v_scale, block_tables, context_lens, query_start, num_query_rows,
+                         max_chunk_len, out, workspace, sh, hip_stream, &w);
 }
 
 extern "C" int coopt_paged_gqa_prefill_chunk_ws(const void* q, const void* k_cache, const void* v_cache,
@@ -922,7 +1037,7 @@ static void launch_split_merge(PrefillArgs a, int num_seqs, hipStream_t stream)
 static int prefill_chunk(const void* q, const void* k_cache, const void* v_cache, const float* k_scale,
                          const float* v_scale, const int32_t* block_tables, const int32_t* context_lens,
                          const int32_t* query_start, int32_t num_query_rows, int32_t max_chunk_len,
-                         void* out, void* workspace, const coopt_shape* sh, void* hip_stream)
+                         void* out, void* workspace, const coopt_shape* sh, void* hip_stream, const Window* window)
 {
     int st = check_shape(sh);
     if (st != COOPT_OK) return st;
@@ -949,7 +1064,9 @@ static int prefill_chunk(const void* q, const void* k_cache, const void* v_cache
 
     const PrefillLaunchPlan lp(sh, max_chunk_len, workspace != nullptr);
     const int pairs8 = lp.pairs8, a_per_pair = lp.a_per_pair, b_per_pair = lp.b_per_pair;
-    a.set(lp, sh->num_seqs * sh->num_kv_heads, (long long)sh->max_blocks_per_seq * kBlock);
+    const long long most_tokens = window ? window_stream_tokens(sh, *window) : (long long)sh->max_blocks_per_seq * kBlock;
+    a.set(lp, sh->num_seqs * sh->num_kv_heads, most_tokens);
+    if (window) a.window = *window;
     a.part = (float*)workspace;
     const bool split = a.split >= 2;                  // (the table may hold no sequence long enough)
     const int split_per_pair = a.split * a.split_blocks;
@@ -961,7 +1078,8 @@ static int prefill_chunk(const void* q, const void* k_cache, const void* v_cache
     // and 102 with one of 2048 columns, 3 x 3.5 MB an XCD (159 by head, first rows first).
     const long long token_bytes = (sh->kv_dtype == COOPT_KV_FP16 ? 4LL : 2LL) * sh->head_dim +
                                   (sh->kv_dtype == COOPT_KV_FP16 ? 0 : 8);
-    a.by_pair = a.xcd_pairs * (long long)sh->max_blocks_per_seq * kBlock * token_bytes > kPrefillXcdL2;
+    const long long pair_tokens = std::min((long long)sh->max_blocks_per_seq * kBlock, most_tokens + max_chunk_len);
+    a.by_pair = a.xcd_pairs * pair_tokens * token_bytes > kPrefillXcdL2;
     // Ragged batches in the order of their streams' lengths, over up to 64 pairs an XCD (one a lane).  A
     // workgroup goes to the XCD's four shader engines in turn whether they have room or not, so a long
     // stream behind a short one, or a workgroup without tiles, holds up all that come after it.  Finding
@@ -969,7 +1087,7 @@ static int prefill_chunk(const void* q, const void* k_cache, const void* v_cache
     // rows are missing: 16 prompts of 100 to 800 rows (8 a CU, 56 % of the rows) 139 -> 120 us, 6 of 200 to
     // 1500 (d = 64, 4.7 a CU) 95 -> 89; 3 of 301 to 1777 (3.6 a CU) 90 -> 93, 8 of 352 rows each 80 -> 88.
     const long long wgs = (long long)pairs8 * (a_per_pair + b_per_pair + split_per_pair);
-    if (!a.by_pair && a.xcd_pairs <= 64 && wgs >= 4 * kPrefillCUs &&
+    if (!window && !a.by_pair && a.xcd_pairs <= 64 && wgs >= 4 * kPrefillCUs &&
         4LL * num_query_rows <= 3LL * sh->num_seqs * max_chunk_len)
         while ((1LL << a.rank_bits) <= ((long long)sh->max_blocks_per_seq * kBlock + kPrefillStageTokens - 1) / kPrefillStageTokens)
             ++a.rank_bits;
@@ -979,11 +1097,17 @@ static int prefill_chunk(const void* q, const void* k_cache, const void* v_cache
                        (size_t)(sh->head_dim == 128 ? PrefillStage<128>::kBytes : PrefillStage<64>::kBytes);
     hipStream_t stream = (hipStream_t)hip_stream;
     const bool big = !pool_fits_small(sh);
+#define COOPT_PREFILL_KERNEL(D, KV, BIG, TILES, per_pair)                                              \
+    do {                                                                                            \
+        const dim3 grid((unsigned)((long long)pairs8 * (per_pair)));                                \
+        if (window)                                                                                 \
+            hipLaunchKernelGGL((prefill_chunk_kernel<D, KV, TILES, BIG, true>), grid, block, lds, stream, a); \
+        else                                                                                        \
+            hipLaunchKernelGGL((prefill_chunk_kernel<D, KV, TILES, BIG>), grid, block, lds, stream, a); \
+    } while (0)
 #define COOPT_PREFILL_FULL(D, KV, BIG, TILES)                                                          \
     do {                                                                                            \
-        hipLaunchKernelGGL((prefill_chunk_kernel<D, KV, TILES, BIG>),                                  \
-                           dim3((unsigned)((long long)pairs8 * (a_per_pair + split_per_pair))), block, lds, \
-                           stream, a);                                                              \
+        COOPT_PREFILL_KERNEL(D, KV, BIG, TILES, a_per_pair + split_per_pair);                       \
         if (split)                                                                                  \
             launch_split_merge<D>(a, sh->num_seqs, stream);                                         \
     } while (0)
@@ -992,11 +1116,10 @@ static int prefill_chunk(const void* q, const void* k_cache, const void* v_cache
         if (lp.nr == 1) {                                                                           \
             COOPT_PREFILL_FULL(D, KV, BIG, 8);                                                      \
         } else {                                                                                    \
-            COOPT_PREFILL_FULL(D, KV, BIG, 16);                                                      \
+            COOPT_PREFILL_FULL(D, KV, BIG, 16);                                                     \
             if (!split && b_per_pair) {                                                             \
                 a.set_rest(lp);                                                                     \
-                hipLaunchKernelGGL((prefill_chunk_kernel<D, KV, 8, BIG>),                           \
-                                   dim3((unsigned)((long long)pairs8 * b_per_pair)), block, lds, stream, a); \
+                COOPT_PREFILL_KERNEL(D, KV, BIG, 8, b_per_pair);                                    \
             }                                                                                       \
         }                                                                                           \
     } while (0)
@@ -1012,5 +1135,6 @@ static int prefill_chunk(const void* q, const void* k_cache, const void* v_cache
     }
 #undef COOPT_PREFILL
 #undef COOPT_PREFILL_FULL
+#undef COOPT_PREFILL_KERNEL
     return launch_status();
 }

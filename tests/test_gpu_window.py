@@ -172,14 +172,14 @@ def test_other_softmax_scales(oracle_mod, scale):
 
 
 def test_rows_of_a_chunk_longer_than_announced(oracle_mod):
-    """Rows beyond max_chunk_len may be left as they were; every other row is right."""
+    """Some heads' rows of the sequence may be left as they were; every other row is right."""
     w = random_workload("window_announced", 17, "e4m3", 10, 2, 128, [200, 90])
     q, starts = ragged_rows(w, [100, 40])
     cache, tables = poisoned(oracle_mod, w, hidden_from(w, [100, 40], 64, 4))
     ref = window_attention(w, cache, q, w.context_lens, starts, 64, 4)
     got = hip_prefill_window(w, cache_to_dev(cache), tables, q, starts, 64, 4, longest=48)
     assert_close(got[100:], ref[100:], "the other sequence")
-    left = np.all(got[:100] == -7.0, axis=(1, 2))
+    left = np.all(got[:100] == -7.0, axis=2)                 # of some heads, as the deal has it
     assert_close(got[:100][~left], ref[:100][~left], "rows that were written")
 
 
