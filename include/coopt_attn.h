@@ -10,7 +10,7 @@
  * Conventions that hold for every entry point
  * -------------------------------------------
  *  - Every pointer argument is a DEVICE pointer owned by the caller, except `const coopt_shape*`
- *    (host) and `hip_stream` (a hipStream_t passed as void*; NULL = the default stream).
+ *    (host), the arrays of layers' pointers of coopt_kv_cache_copy_blocks (host) and `hip_stream` (a hipStream_t passed as void*; NULL = the default stream).
  *  - Unless a comment says otherwise the library allocates nothing, frees nothing, copies nothing
  *    to the host and never synchronises: kernels are enqueued on `hip_stream` and the call returns.
  *  - Return value: COOPT_OK (0) or a negative coopt_status.  Arguments are validated before the
@@ -467,6 +467,99 @@ int coopt_paged_gqa_prefill_chunk_window(const void* q, const void* k_cache, con
                                          int32_t max_chunk_len, int32_t window, int32_t num_sinks, void* out,
                                          void* workspace, size_t workspace_bytes, const coopt_shape* shape,
                                          void* hip_stream);
+
+/*
+ * The pool's blocks
+ * -----------------
+ * Who holds a block, which ones are free, and moving them: what a server does between the launches above when
+ * sequences grow, share a prompt, end, or leave blocks behind a window.  It works on device memory of the
+ * caller's, so that a step needs no copy to the host:
+ *   block_tables, context_lens   as above, but written to
+ *   ref_counts [num_blocks] int32       how many table entries name the block
+ *   free_map [ceil(num_blocks/32)] uint32   bit b % 32 of word b / 32 is set iff block b is free (ref_counts[b] is 0);
+ *                                       bits from num_blocks on are 0
+ * Sequence s holds the entries b < ceil(context_lens[s]/16) of its row that name a block (0 <= entry < num_blocks);
+ * -1 stands where a block was given back.  Other entries may hold anything and are neither read nor written.
+ * Blocks are always taken lowest number first, so the results are the same every time.  Calls on one pool must
+ * be ordered, with each other and with the launches that read or write its blocks.  A negative sequence index in
+ * a list is left out, as a negative slot is.  num_q_heads, head_dim, kv_dtype and softmax_scale of the shape do not
+ * matter, but have to be valid.
+ *   result (device, int32 [1])   0: done; n > 0: n blocks too few were free; -1: an argument in device memory
+ *                                out of its range.  Where it is not 0 nothing has been changed, and slots and
+ *                                copies are all -1, so that the calls which take them do nothing.
+ *   workspace  coopt_kv_blocks_workspace_bytes(shape) bytes, 16-byte aligned, contents undefined before and after
+ *
+ * init: ref_counts and free_map from tables and lengths (lengths of 0: an empty pool).
+ */
+size_t coopt_kv_blocks_workspace_bytes(const coopt_shape* shape);
+int coopt_kv_blocks_init(const int32_t* block_tables, const int32_t* context_lens, int32_t* ref_counts,
+                         uint32_t* free_map, const coopt_shape* shape, void* hip_stream);
+
+/*
+ * reserve: room for new tokens.  Sequence s gets query_start[s+1] - query_start[s] of them (as the rows of a prefill;
+ * query_start [num_seqs+1] from 0, increasing, its last at most num_query_rows) -- or, with query_start NULL, one where
+ * context_lens[s] > 0 and none elsewhere, row s being sequence s's (num_query_rows >= num_seqs).  New table entries
+ * name free blocks (of sequences, then of entries, in order), context_lens counts the new tokens, and
+ * slot_mapping [num_query_rows] int64 gets every row's slot (-1 for a sequence without tokens; rows from
+ * query_start[num_seqs] on are left as they were): the arguments of the cache write and the attention that follow.
+ * result -1: a sequence would outgrow its row of the table, or query_start is none.  A sequence that grows inside its
+ * last block must hold it alone (as after fork).
+ */
+int coopt_kv_blocks_reserve(const int32_t* query_start, int32_t num_query_rows, int32_t* block_tables,
+                            int32_t* context_lens, int32_t* ref_counts, uint32_t* free_map,
+                            int64_t* slot_mapping, int32_t* result, void* workspace, size_t workspace_bytes,
+                            const coopt_shape* shape, void* hip_stream);
+
+/*
+ * fork: sequence children[i] goes on from the tokens of parents[i] (int32 [num_forks], num_forks <= num_seqs).  Full
+ * blocks are shared; a last block that is not full gets a block of its own, into which
+ * coopt_kv_cache_copy_blocks has to copy it before either grows: copies [num_forks][2] int32 gets (from, to),
+ * or (-1, -1) where there is nothing to copy.  Several children may have one parent.  result -1: an index >= num_seqs, a
+ * child that is its own parent, holds tokens (context_lens != 0) or is named twice.
+ */
+int coopt_kv_blocks_fork(const int32_t* parents, const int32_t* children, int32_t num_forks,
+                         int32_t* block_tables, int32_t* context_lens, int32_t* ref_counts,
+                         uint32_t* free_map, int32_t* copies, int32_t* result, void* workspace,
+                         size_t workspace_bytes, const coopt_shape* shape, void* hip_stream);
+
+/*
+ * free: the listed sequences (int32 [num_listed], at most 2^20; one listed twice is freed once, an index >= num_seqs
+ * is left out) hold nothing any more: context_lens 0, their table entries as they were.
+ */
+int coopt_kv_blocks_free(const int32_t* seqs, int32_t num_listed, const int32_t* block_tables,
+                         int32_t* context_lens, int32_t* ref_counts, uint32_t* free_map,
+                         const coopt_shape* shape, void* hip_stream);
+
+/*
+ * free outside the window: of every sequence the blocks that no token at position context_lens[s] - 1 or after sees
+ * through the window (all their tokens j have num_sinks <= j <= context_lens[s] - 1 - window); their entries become -1.
+ * Calls on a sequence must all have the same num_sinks, and only they and fork write -1 into its row: the walk ends
+ * where an earlier call's work begins.
+ */
+int coopt_kv_blocks_free_outside_window(int32_t* block_tables, const int32_t* context_lens,
+                                        int32_t* ref_counts, uint32_t* free_map, int32_t window,
+                                        int32_t num_sinks, const coopt_shape* shape, void* hip_stream);
+
+/*
+ * compact: the n blocks in use become blocks 0 .. n-1.  Those numbered n and above are renumbered, in order, to the
+ * free ones below n in order; copies [num_blocks/2][2] int32 gets (from, to) of the first num_copies (device, int32
+ * [1]) of them, which coopt_kv_cache_copy_blocks has to carry out before the blocks are used again.
+ */
+int coopt_kv_blocks_compact(int32_t* block_tables, const int32_t* context_lens, int32_t* ref_counts,
+                            uint32_t* free_map, int32_t* copies, int32_t* num_copies, void* workspace,
+                            size_t workspace_bytes, const coopt_shape* shape, void* hip_stream);
+
+/*
+ * Copies blocks inside the pools of num_layers layers in one launch per 64 layers: for every pair (from, to) of copies
+ * [max_copies][2] -- of the first *num_copies (device, int32 [1]) where that is not NULL -- the K, V and scales of all
+ * heads.  A pair that names no block (-1) is left out.  No block may be written twice, or written and read, in one call.
+ *   k_caches .. v_scales   HOST arrays of num_layers device pointers, read during the call only; the scales' are
+ *                          NULL or ignored for fp16 caches
+ */
+int coopt_kv_cache_copy_blocks(void* const* k_caches, void* const* v_caches, float* const* k_scales,
+                               float* const* v_scales, int32_t num_layers, const int32_t* copies,
+                               int32_t max_copies, const int32_t* num_copies, const coopt_shape* shape,
+                               void* hip_stream);
 
 /*
  * Dequantising gather (the read half of Opt-KV, Eq. 6; the paper's gather_cached_kv): contiguous

@@ -13,4 +13,5 @@ from .binding import (  # noqa: F401
     paged_gqa_decode_scheduled, paged_gqa_decode_split, paged_gqa_decode_step,
     paged_gqa_prefill_chunk, paged_gqa_prefill_chunk_ws, paged_gqa_reduce, prefill_workspace_bytes,
     decode_window_workspace_bytes, paged_gqa_decode_window, paged_gqa_decode_window_step, paged_gqa_prefill_chunk_window, prefill_window_workspace_bytes,
-    status_string)
+    kv_blocks_compact, kv_blocks_fork, kv_blocks_free, kv_blocks_free_outside_window, kv_blocks_init, kv_blocks_reserve,
+    kv_blocks_workspace_bytes, kv_cache_copy_blocks, status_string)

@@ -39,6 +39,9 @@ EXPORTS = [
     "coopt_paged_gqa_prefill_chunk_ws", "coopt_prefill_workspace_bytes",
     "coopt_paged_gqa_decode_window", "coopt_decode_window_workspace_bytes", "coopt_paged_gqa_decode_window_step",
     "coopt_paged_gqa_prefill_chunk_window", "coopt_prefill_window_workspace_bytes",
+    "coopt_kv_blocks_workspace_bytes", "coopt_kv_blocks_init", "coopt_kv_blocks_reserve", "coopt_kv_blocks_fork",
+    "coopt_kv_blocks_free", "coopt_kv_blocks_free_outside_window", "coopt_kv_blocks_compact",
+    "coopt_kv_cache_copy_blocks",
 ]
 
 
@@ -109,6 +112,15 @@ def load_library():
                                                              shp, vp]
         lib.coopt_prefill_window_workspace_bytes.argtypes = [shp, i32, i32, i32]
         lib.coopt_prefill_window_workspace_bytes.restype = sz
+        lib.coopt_kv_blocks_workspace_bytes.argtypes = [shp]
+        lib.coopt_kv_blocks_workspace_bytes.restype = sz
+        lib.coopt_kv_blocks_init.argtypes = [vp, vp, vp, vp, shp, vp]
+        lib.coopt_kv_blocks_reserve.argtypes = [vp, i32, vp, vp, vp, vp, vp, vp, vp, sz, shp, vp]
+        lib.coopt_kv_blocks_fork.argtypes = [vp, vp, i32, vp, vp, vp, vp, vp, vp, vp, sz, shp, vp]
+        lib.coopt_kv_blocks_free.argtypes = [vp, i32, vp, vp, vp, vp, shp, vp]
+        lib.coopt_kv_blocks_free_outside_window.argtypes = [vp, vp, vp, vp, i32, i32, shp, vp]
+        lib.coopt_kv_blocks_compact.argtypes = [vp, vp, vp, vp, vp, vp, vp, sz, shp, vp]
+        lib.coopt_kv_cache_copy_blocks.argtypes = [vp, vp, vp, vp, i32, vp, i32, vp, shp, vp]
         lib.coopt_gather_cached_kv.argtypes = [vp, vp, vp, vp, vp, i32, i32, i32, vp, vp, shp, vp]
         lib.coopt_decode_schedule_bytes.argtypes = [shp, plp]
         lib.coopt_decode_schedule_bytes.restype = sz
@@ -123,7 +135,7 @@ def load_library():
         for name in EXPORTS:
             if name not in ("coopt_decode_workspace_bytes", "coopt_decode_schedule_bytes",
                             "coopt_prefill_workspace_bytes", "coopt_decode_window_workspace_bytes",
-                            "coopt_prefill_window_workspace_bytes", "coopt_status_string", "coopt_default_decode_plan",
+                            "coopt_prefill_window_workspace_bytes", "coopt_kv_blocks_workspace_bytes", "coopt_status_string", "coopt_default_decode_plan",
                             "coopt_decode_builtin_workspace_bytes"):
                 getattr(lib, name).restype = ctypes.c_int
         _lib = lib
@@ -669,3 +681,102 @@ def gather_cached_kv(k_cache, v_cache, k_scale, v_scale, block_tables, seq: int,
         int(tok_begin), int(tok_end), _dev(k_out, "k_out", what, elem=2, min_bytes=rows),
         _dev(v_out, "v_out", what, elem=2, min_bytes=rows), ctypes.byref(shape),
         _stream(stream))
+
+
+# ---------------------------------------------------------------- the pool's blocks
+
+def kv_blocks_workspace_bytes(shape: Shape) -> int:
+    return int(load_library().coopt_kv_blocks_workspace_bytes(ctypes.byref(shape)))
+
+
+def _block_state(block_tables, context_lens, ref_counts, free_map, shape: Shape, what: str):
+    z = _sizes(shape)
+    return (_dev(block_tables, "block_tables", what, dtype=_i32(), min_bytes=z["tables"]),
+            _dev(context_lens, "context_lens", what, dtype=_i32(), min_bytes=z["lens"]),
+            _dev(ref_counts, "ref_counts", what, dtype=_i32(), min_bytes=4 * shape.num_blocks),
+            _dev(free_map, "free_map", what, elem=4, min_bytes=(shape.num_blocks + 31) // 32 * 4))
+
+
+def kv_blocks_init(block_tables, context_lens, ref_counts, free_map, shape: Shape, stream=None) -> None:
+    """ref_counts and free_map (4-byte words) from the tables and lengths."""
+    _call("coopt_kv_blocks_init",
+          *_block_state(block_tables, context_lens, ref_counts, free_map, shape, "kv_blocks_init"),
+          ctypes.byref(shape), _stream(stream))
+
+
+def kv_blocks_reserve(query_start, num_query_rows: int, block_tables, context_lens, ref_counts, free_map,
+                      slot_mapping, result, workspace, shape: Shape, stream=None) -> None:
+    """Blocks and slots for new tokens: query_start's rows, or (None) one for every sequence that holds tokens.
+    result: int32 [1], 0 once done; see the header for what else it may say."""
+    what = "kv_blocks_reserve"
+    state = _block_state(block_tables, context_lens, ref_counts, free_map, shape, what)
+    pws, nws = _sized_workspace(workspace, kv_blocks_workspace_bytes(shape), what)
+    _call("coopt_kv_blocks_reserve",
+          _dev(query_start, "query_start", what, dtype=_i32(), min_bytes=4 * shape.num_seqs + 4, optional=True),
+          int(num_query_rows), *state,
+          _dev(slot_mapping, "slot_mapping", what, dtype=_i64(), min_bytes=8 * int(num_query_rows)),
+          _dev(result, "result", what, dtype=_i32(), min_bytes=4), pws, nws, ctypes.byref(shape), _stream(stream))
+
+
+def kv_blocks_fork(parents, children, block_tables, context_lens, ref_counts, free_map, copies, result, workspace,
+                   shape: Shape, stream=None) -> None:
+    """children[i] goes on from parents[i]'s tokens; copies [len(parents)][2] are for kv_cache_copy_blocks."""
+    what = "kv_blocks_fork"
+    state = _block_state(block_tables, context_lens, ref_counts, free_map, shape, what)
+    pws, nws = _sized_workspace(workspace, kv_blocks_workspace_bytes(shape), what)
+    pp, n = _dev(parents, "parents", what, dtype=_i32()), parents.numel()
+    _call("coopt_kv_blocks_fork",
+          pp, _dev(children, "children", what, dtype=_i32(), min_bytes=4 * n), n, *state,
+          _dev(copies, "copies", what, dtype=_i32(), min_bytes=8 * n), _dev(result, "result", what, dtype=_i32(), min_bytes=4),
+          pws, nws, ctypes.byref(shape), _stream(stream))
+
+
+def kv_blocks_free(seqs, block_tables, context_lens, ref_counts, free_map, shape: Shape, stream=None) -> None:
+    """The listed sequences hold nothing any more."""
+    what = "kv_blocks_free"
+    state = _block_state(block_tables, context_lens, ref_counts, free_map, shape, what)
+    _call("coopt_kv_blocks_free", _dev(seqs, "seqs", what, dtype=_i32()), seqs.numel(), *state, ctypes.byref(shape),
+          _stream(stream))
+
+
+def kv_blocks_free_outside_window(block_tables, context_lens, ref_counts, free_map, window: int, num_sinks: int,
+                                  shape: Shape, stream=None) -> None:
+    """Every sequence's blocks that lie behind the window for good."""
+    state = _block_state(block_tables, context_lens, ref_counts, free_map, shape, "kv_blocks_free_outside_window")
+    _call("coopt_kv_blocks_free_outside_window", *state, int(window), int(num_sinks), ctypes.byref(shape), _stream(stream))
+
+
+def kv_blocks_compact(block_tables, context_lens, ref_counts, free_map, copies, num_copies, workspace, shape: Shape,
+                      stream=None) -> None:
+    """The blocks in use to the front of the pool; copies [num_blocks // 2][2] and num_copies are for
+    kv_cache_copy_blocks."""
+    what = "kv_blocks_compact"
+    state = _block_state(block_tables, context_lens, ref_counts, free_map, shape, what)
+    pws, nws = _sized_workspace(workspace, kv_blocks_workspace_bytes(shape), what)
+    _call("coopt_kv_blocks_compact",
+          *state, _dev(copies, "copies", what, dtype=_i32(), min_bytes=8 * (shape.num_blocks // 2)),
+          _dev(num_copies, "num_copies", what, dtype=_i32(), min_bytes=4), pws, nws, ctypes.byref(shape), _stream(stream))
+
+
+def kv_cache_copy_blocks(k_caches, v_caches, k_scales, v_scales, copies, num_copies, shape: Shape, stream=None) -> None:
+    """Copies the blocks of the pairs (from, to) in the pools of all layers: k_caches .. v_scales are a layer's
+    tensor each, or lists of the layers' (the scales None for fp16 caches); num_copies None: all pairs."""
+    what = "kv_cache_copy_blocks"
+    z = _sizes(shape)
+
+    def layers(pools):
+        return [pools] if pools is None or hasattr(pools, "data_ptr") else list(pools)
+    n = len(layers(k_caches))
+
+    def pointers(pools, name, need, optional=False):
+        if optional and pools is None:
+            return None
+        pools = layers(pools)
+        if len(pools) != n:
+            raise CooptError(f"{what}: {name}: {len(pools)} layers, expected {n}")
+        return (ctypes.c_void_p * n)(*(_dev(p, name, what, need) for p in pools))
+    _call("coopt_kv_cache_copy_blocks",
+          pointers(k_caches, "k_caches", z["cache"]), pointers(v_caches, "v_caches", z["cache"]),
+          pointers(k_scales, "k_scales", z["scale"], not z["scaled"]), pointers(v_scales, "v_scales", z["scale"], not z["scaled"]),
+          n, _dev(copies, "copies", what, dtype=_i32()), copies.numel() // 2,
+          _dev(num_copies, "num_copies", what, dtype=_i32(), min_bytes=4, optional=True), ctypes.byref(shape), _stream(stream))

@@ -22,7 +22,7 @@ CSRC = os.path.join(HERE, "csrc")
 BUILD = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libcoopt_attn.so")
 PROBE_LIB = os.path.join(HERE, "libcoopt_probe.so")      # measurement aid, not the product
-SOURCES = ["kv_write.hip", "decode.hip", "decode_flat.hip", "prefill.hip", "gather.hip"]
+SOURCES = ["kv_write.hip", "decode.hip", "decode_flat.hip", "prefill.hip", "gather.hip", "blocks.hip"]
 PROBE_SOURCES = ["probe.hip"]
 BINDING = os.path.join(HERE, "_binding" + (sysconfig.get_config_var("EXT_SUFFIX") or ".so"))
 BINDING_SOURCE = "binding_native.cpp"                    # host code: tensors to pointers, no kernel
