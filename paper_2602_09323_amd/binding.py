@@ -198,7 +198,10 @@ def _bind_native():
     names = ("kv_cache_write_fp8", "kv_cache_write_fp16", "paged_gqa_decode", "paged_gqa_decode_step",
              "decode_schedule_prepare", "paged_gqa_decode_scheduled", "paged_gqa_decode_partitioned",
              "paged_gqa_reduce", "paged_gqa_prefill_chunk_ws", "gather_cached_kv", "decode_workspace_bytes",
-             "decode_schedule_bytes", "prefill_workspace_bytes")
+             "decode_schedule_bytes", "prefill_workspace_bytes", "paged_gqa_decode_window", "paged_gqa_decode_window_step",
+             "paged_gqa_prefill_chunk_window", "decode_window_workspace_bytes", "prefill_window_workspace_bytes",
+             "kv_blocks_reserve", "kv_blocks_fork", "kv_blocks_free", "kv_blocks_free_outside_window", "kv_blocks_compact",
+             "kv_cache_copy_blocks", "kv_blocks_workspace_bytes")
     _binding.bind(tuple(ctypes.cast(getattr(_lib, "coopt_" + n), ctypes.c_void_p).value for n in names),
                   Shape, DecodePlan, device, raw)
     return _binding
@@ -569,6 +572,10 @@ def paged_gqa_decode_window(q, k_cache, v_cache, k_scale, v_scale, block_tables,
                             num_sinks: int, out, workspace, shape: Shape, stream=None) -> None:
     """One new token per sequence attends to its last ``window`` tokens and the first ``num_sinks``.
     workspace: a device buffer of at least decode_window_workspace_bytes(...) bytes (None where that is 0)."""
+    fast = _fast()
+    if fast is not None and _entered(fast.window(q, k_cache, v_cache, k_scale, v_scale, block_tables, context_lens, window, num_sinks,
+                                                 out, workspace, shape, stream), "coopt_paged_gqa_decode_window"):
+        return
     what = "paged_gqa_decode_window"
     z = _sizes(shape)
     ins = _decode_inputs(q, k_cache, v_cache, k_scale, v_scale, block_tables, context_lens, z, what)
@@ -582,6 +589,10 @@ def paged_gqa_decode_window_step(k, v, slot_mapping, q, k_cache, v_cache, k_scal
                                  context_lens, window: int, num_sinks: int, out, workspace, shape: Shape,
                                  stream=None) -> None:
     """The write of one new token per sequence and paged_gqa_decode_window in one call."""
+    fast = _fast()
+    if fast is not None and _entered(fast.window_step(k, v, slot_mapping, q, k_cache, v_cache, k_scale, v_scale, block_tables, context_lens,
+                                                      window, num_sinks, out, workspace, shape, stream), "coopt_paged_gqa_decode_window_step"):
+        return
     what = "paged_gqa_decode_window_step"
     z = _sizes(shape)
     pk, pv, ps, T = _new_rows(k, v, slot_mapping, z, what)
@@ -604,18 +615,22 @@ def paged_gqa_prefill_chunk_window(q, k_cache, v_cache, k_scale, v_scale, block_
                                    num_sinks: int, out, workspace, shape: Shape, stream=None) -> None:
     """Every row of the chunks through its own window.  workspace: at least prefill_window_workspace_bytes(...)
     bytes (None where that is 0)."""
+    fast = _fast()
+    if fast is not None and _entered(fast.window_prefill(q, k_cache, v_cache, k_scale, v_scale, block_tables, context_lens, query_start,
+                                                         num_query_rows, max_chunk_len, window, num_sinks, out, workspace, shape, stream), "coopt_paged_gqa_prefill_chunk_window"):
+        return
     what = "paged_gqa_prefill_chunk_window"
     z = _sizes(shape)
     rows_bytes = int(num_query_rows) * shape.num_q_heads * shape.head_dim * 2
+    ins = (_dev(q, "q", what, elem=2, min_bytes=rows_bytes),
+           *_cache_ptrs(k_cache, v_cache, k_scale, v_scale, z),
+           _dev(block_tables, "block_tables", what, dtype=_i32(), min_bytes=z["tables"]),
+           _dev(context_lens, "context_lens", what, dtype=_i32(), min_bytes=z["lens"]),
+           _dev(query_start, "query_start", what, dtype=_i32(), min_bytes=z["lens"] + 4))
     need = prefill_window_workspace_bytes(shape, max_chunk_len, window, num_sinks)
     pws, nws = _sized_workspace(workspace, need, what)
     _call("coopt_paged_gqa_prefill_chunk_window",
-          _dev(q, "q", what, elem=2, min_bytes=rows_bytes),
-          *_cache_ptrs(k_cache, v_cache, k_scale, v_scale, z),
-          _dev(block_tables, "block_tables", what, dtype=_i32(), min_bytes=z["tables"]),
-          _dev(context_lens, "context_lens", what, dtype=_i32(), min_bytes=z["lens"]),
-          _dev(query_start, "query_start", what, dtype=_i32(), min_bytes=z["lens"] + 4),
-          int(num_query_rows), int(max_chunk_len), int(window), int(num_sinks),
+          *ins, int(num_query_rows), int(max_chunk_len), int(window), int(num_sinks),
           _dev(out, "out", what, elem=2, min_bytes=rows_bytes), pws, nws, ctypes.byref(shape), _stream(stream))
 
 
@@ -708,6 +723,10 @@ def kv_blocks_reserve(query_start, num_query_rows: int, block_tables, context_le
                       slot_mapping, result, workspace, shape: Shape, stream=None) -> None:
     """Blocks and slots for new tokens: query_start's rows, or (None) one for every sequence that holds tokens.
     result: int32 [1], 0 once done; see the header for what else it may say."""
+    fast = _fast()
+    if fast is not None and _entered(fast.reserve(query_start, num_query_rows, block_tables, context_lens, ref_counts, free_map, slot_mapping, result,
+                                                  workspace, shape, stream), "coopt_kv_blocks_reserve"):
+        return
     what = "kv_blocks_reserve"
     state = _block_state(block_tables, context_lens, ref_counts, free_map, shape, what)
     pws, nws = _sized_workspace(workspace, kv_blocks_workspace_bytes(shape), what)
@@ -721,6 +740,10 @@ def kv_blocks_reserve(query_start, num_query_rows: int, block_tables, context_le
 def kv_blocks_fork(parents, children, block_tables, context_lens, ref_counts, free_map, copies, result, workspace,
                    shape: Shape, stream=None) -> None:
     """children[i] goes on from parents[i]'s tokens; copies [len(parents)][2] are for kv_cache_copy_blocks."""
+    fast = _fast()
+    if fast is not None and _entered(fast.fork_blocks(parents, children, block_tables, context_lens, ref_counts, free_map, copies, result, workspace,
+                                                      shape, stream), "coopt_kv_blocks_fork"):
+        return
     what = "kv_blocks_fork"
     state = _block_state(block_tables, context_lens, ref_counts, free_map, shape, what)
     pws, nws = _sized_workspace(workspace, kv_blocks_workspace_bytes(shape), what)
@@ -733,6 +756,9 @@ def kv_blocks_fork(parents, children, block_tables, context_lens, ref_counts, fr
 
 def kv_blocks_free(seqs, block_tables, context_lens, ref_counts, free_map, shape: Shape, stream=None) -> None:
     """The listed sequences hold nothing any more."""
+    fast = _fast()
+    if fast is not None and _entered(fast.free_seqs(seqs, block_tables, context_lens, ref_counts, free_map, shape, stream), "coopt_kv_blocks_free"):
+        return
     what = "kv_blocks_free"
     state = _block_state(block_tables, context_lens, ref_counts, free_map, shape, what)
     _call("coopt_kv_blocks_free", _dev(seqs, "seqs", what, dtype=_i32()), seqs.numel(), *state, ctypes.byref(shape),
@@ -742,6 +768,9 @@ def kv_blocks_free(seqs, block_tables, context_lens, ref_counts, free_map, shape
 def kv_blocks_free_outside_window(block_tables, context_lens, ref_counts, free_map, window: int, num_sinks: int,
                                   shape: Shape, stream=None) -> None:
     """Every sequence's blocks that lie behind the window for good."""
+    fast = _fast()
+    if fast is not None and _entered(fast.free_window(block_tables, context_lens, ref_counts, free_map, window, num_sinks, shape, stream), "coopt_kv_blocks_free_outside_window"):
+        return
     state = _block_state(block_tables, context_lens, ref_counts, free_map, shape, "kv_blocks_free_outside_window")
     _call("coopt_kv_blocks_free_outside_window", *state, int(window), int(num_sinks), ctypes.byref(shape), _stream(stream))
 
@@ -750,6 +779,9 @@ def kv_blocks_compact(block_tables, context_lens, ref_counts, free_map, copies, 
                       stream=None) -> None:
     """The blocks in use to the front of the pool; copies [num_blocks // 2][2] and num_copies are for
     kv_cache_copy_blocks."""
+    fast = _fast()
+    if fast is not None and _entered(fast.compact(block_tables, context_lens, ref_counts, free_map, copies, num_copies, workspace, shape, stream), "coopt_kv_blocks_compact"):
+        return
     what = "kv_blocks_compact"
     state = _block_state(block_tables, context_lens, ref_counts, free_map, shape, what)
     pws, nws = _sized_workspace(workspace, kv_blocks_workspace_bytes(shape), what)
@@ -761,6 +793,9 @@ def kv_blocks_compact(block_tables, context_lens, ref_counts, free_map, copies, 
 def kv_cache_copy_blocks(k_caches, v_caches, k_scales, v_scales, copies, num_copies, shape: Shape, stream=None) -> None:
     """Copies the blocks of the pairs (from, to) in the pools of all layers: k_caches .. v_scales are a layer's
     tensor each, or lists of the layers' (the scales None for fp16 caches); num_copies None: all pairs."""
+    fast = _fast()
+    if fast is not None and _entered(fast.copy_blocks(k_caches, v_caches, k_scales, v_scales, copies, num_copies, shape, stream), "coopt_kv_cache_copy_blocks"):
+        return
     what = "kv_cache_copy_blocks"
     z = _sizes(shape)
 

@@ -13,6 +13,8 @@
 #include <ATen/PythonTorchFunctionTLS.h>
 #include <torch/csrc/autograd/python_variable.h>
 
+#include <vector>
+
 #include "coopt_attn.h"
 
 namespace {
@@ -35,6 +37,18 @@ struct {
     decltype(&coopt_decode_workspace_bytes) workspace_bytes;
     decltype(&coopt_decode_schedule_bytes) schedule_bytes;
     decltype(&coopt_prefill_workspace_bytes) prefill_bytes;
+    decltype(&coopt_paged_gqa_decode_window) window;
+    decltype(&coopt_paged_gqa_decode_window_step) window_step;
+    decltype(&coopt_paged_gqa_prefill_chunk_window) window_prefill;
+    decltype(&coopt_decode_window_workspace_bytes) window_bytes;
+    decltype(&coopt_prefill_window_workspace_bytes) window_prefill_bytes;
+    decltype(&coopt_kv_blocks_reserve) reserve;
+    decltype(&coopt_kv_blocks_fork) fork;
+    decltype(&coopt_kv_blocks_free) free_seqs;
+    decltype(&coopt_kv_blocks_free_outside_window) free_window;
+    decltype(&coopt_kv_blocks_compact) compact;
+    decltype(&coopt_kv_cache_copy_blocks) copy_blocks;
+    decltype(&coopt_kv_blocks_workspace_bytes) blocks_bytes;
     PyObject *shape_class, *plan_class, *current_device, *raw_stream;
 } lib = {};
 
@@ -372,20 +386,216 @@ PyObject* gather(PyObject*, PyObject* const* a, Py_ssize_t n)
     });
 }
 
+// A caller's workspace of at least `need` bytes, or None where none is needed.
+struct Workspace {
+    void* at = nullptr;
+    size_t bytes = 0;
+    Workspace(PyObject* o, size_t need)
+    {
+        if (o == Py_None && need == 0) return;
+        const Tensor w(o, (wide)need, 0);
+        at = w.at;
+        bytes = (size_t)w.bytes;
+    }
+};
+
+PyObject* window(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+    return guarded<13>(n, [&] {
+        const Shape sh(a[11]);
+        const Inputs in(a, sh);
+        const int32_t size = small_int(a[7]), sinks = small_int(a[8]);
+        const Tensor out(a[9], sh.q, 2);
+        const Workspace ws(a[10], lib.window_bytes(&sh, size, sinks));
+        void* s = stream_of(a[12]);
+        return unlocked([&] {
+            return lib.window(in.q.at, in.c.k, in.c.v, in.c.ks, in.c.vs, in.tables.as<int32_t>(), in.lens.as<int32_t>(), size, sinks,
+                              out.at, ws.at, ws.bytes, &sh, s);
+        });
+    });
+}
+
+PyObject* window_step(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+    return guarded<16>(n, [&] {
+        const Shape sh(a[14]);
+        const NewRows r(a, sh);
+        if (r.slots.numel < sh.num_seqs) throw Decline();
+        const Inputs in(a + 3, sh);
+        const int32_t size = small_int(a[10]), sinks = small_int(a[11]);
+        const Tensor out(a[12], sh.q, 2);
+        const Workspace ws(a[13], lib.window_bytes(&sh, size, sinks));
+        void* s = stream_of(a[15]);
+        return unlocked([&] {
+            return lib.window_step(r.k, r.v, r.slots.as<int64_t>(), in.q.at, in.c.k, in.c.v, in.c.ks, in.c.vs, in.tables.as<int32_t>(),
+                                   in.lens.as<int32_t>(), size, sinks, out.at, ws.at, ws.bytes, &sh, s);
+        });
+    });
+}
+
+PyObject* window_prefill(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+    return guarded<16>(n, [&] {
+        const Shape sh(a[14]);
+        const int32_t rows = small_int(a[8]), longest = small_int(a[9]), size = small_int(a[10]), sinks = small_int(a[11]);
+        const wide rows_bytes = (wide)rows * sh.num_q_heads * sh.head_dim * 2;
+        const Tensor q(a[0], rows_bytes, 2);
+        const Cache c(a + 1, sh);
+        const Tensor tables(a[5], sh.tables, c10::kInt), lens(a[6], sh.lens, c10::kInt), starts(a[7], sh.lens + 4, c10::kInt);
+        const Tensor out(a[12], rows_bytes, 2);
+        const Workspace ws(a[13], lib.window_prefill_bytes(&sh, longest, size, sinks));
+        void* s = stream_of(a[15]);
+        return unlocked([&] {
+            return lib.window_prefill(q.at, c.k, c.v, c.ks, c.vs, tables.as<int32_t>(), lens.as<int32_t>(), starts.as<int32_t>(),
+                                      rows, longest, size, sinks, out.at, ws.at, ws.bytes, &sh, s);
+        });
+    });
+}
+
+// tables, lengths, reference counts and map, in this order
+struct Blocks {
+    Tensor tables, lens, refs, free;
+    Blocks(PyObject* const* a, const Shape& sh)
+        : tables(a[0], sh.tables, c10::kInt), lens(a[1], sh.lens, c10::kInt), refs(a[2], (wide)sh.num_blocks * 4, c10::kInt),
+          free(a[3], ((wide)sh.num_blocks + 31) / 32 * 4, 4) {}
+};
+
+// A list of indices: its length fits an int.
+struct Indices : Tensor {
+    int32_t n;
+    explicit Indices(PyObject* o) : Tensor(o, 0, c10::kInt)
+    {
+        if (numel > INT32_MAX) throw Decline();
+        n = (int32_t)numel;
+    }
+};
+
+PyObject* reserve(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+    return guarded<11>(n, [&] {
+        const Shape sh(a[9]);
+        const Blocks b(a + 2, sh);
+        const Workspace ws(a[8], lib.blocks_bytes(&sh));
+        int32_t* starts = a[0] == Py_None ? nullptr : Tensor(a[0], sh.lens + 4, c10::kInt).as<int32_t>();
+        const int32_t rows = small_int(a[1]);
+        const Tensor slots(a[6], (wide)rows * 8, c10::kLong), result(a[7], 4, c10::kInt);
+        void* s = stream_of(a[10]);
+        return unlocked([&] {
+            return lib.reserve(starts, rows, b.tables.as<int32_t>(), b.lens.as<int32_t>(), b.refs.as<int32_t>(), b.free.as<uint32_t>(),
+                               slots.as<int64_t>(), result.as<int32_t>(), ws.at, ws.bytes, &sh, s);
+        });
+    });
+}
+
+PyObject* fork_blocks(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+    return guarded<11>(n, [&] {
+        const Shape sh(a[9]);
+        const Blocks b(a + 2, sh);
+        const Workspace ws(a[8], lib.blocks_bytes(&sh));
+        const Indices parents(a[0]);
+        const Tensor children(a[1], (wide)parents.n * 4, c10::kInt), copies(a[6], (wide)parents.n * 8, c10::kInt), result(a[7], 4, c10::kInt);
+        void* s = stream_of(a[10]);
+        return unlocked([&] {
+            return lib.fork(parents.as<int32_t>(), children.as<int32_t>(), parents.n, b.tables.as<int32_t>(), b.lens.as<int32_t>(),
+                            b.refs.as<int32_t>(), b.free.as<uint32_t>(), copies.as<int32_t>(), result.as<int32_t>(), ws.at, ws.bytes, &sh, s);
+        });
+    });
+}
+
+PyObject* free_seqs(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+    return guarded<7>(n, [&] {
+        const Shape sh(a[5]);
+        const Blocks b(a + 1, sh);
+        const Indices seqs(a[0]);
+        void* s = stream_of(a[6]);
+        return unlocked([&] {
+            return lib.free_seqs(seqs.as<int32_t>(), seqs.n, b.tables.as<int32_t>(), b.lens.as<int32_t>(), b.refs.as<int32_t>(),
+                                 b.free.as<uint32_t>(), &sh, s);
+        });
+    });
+}
+
+PyObject* free_window(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+    return guarded<8>(n, [&] {
+        const Shape sh(a[6]);
+        const Blocks b(a, sh);
+        const int32_t size = small_int(a[4]), sinks = small_int(a[5]);
+        void* s = stream_of(a[7]);
+        return unlocked([&] {
+            return lib.free_window(b.tables.as<int32_t>(), b.lens.as<int32_t>(), b.refs.as<int32_t>(), b.free.as<uint32_t>(), size, sinks, &sh, s);
+        });
+    });
+}
+
+PyObject* compact(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+    return guarded<9>(n, [&] {
+        const Shape sh(a[7]);
+        const Blocks b(a, sh);
+        const Workspace ws(a[6], lib.blocks_bytes(&sh));
+        const Tensor copies(a[4], (wide)(sh.num_blocks / 2) * 8, c10::kInt), count(a[5], 4, c10::kInt);
+        void* s = stream_of(a[8]);
+        return unlocked([&] {
+            return lib.compact(b.tables.as<int32_t>(), b.lens.as<int32_t>(), b.refs.as<int32_t>(), b.free.as<uint32_t>(), copies.as<int32_t>(),
+                               count.as<int32_t>(), ws.at, ws.bytes, &sh, s);
+        });
+    });
+}
+
+// Pointers of a list of tensors (the layers' pools); empty for None.
+std::vector<void*> layers(PyObject* o, wide need)
+{
+    std::vector<void*> at;
+    if (o == Py_None) return at;
+    if (!PyList_CheckExact(o)) {
+        at.push_back(Tensor(o, need, 0).at);
+        return at;
+    }
+    for (Py_ssize_t i = 0; i < PyList_GET_SIZE(o); ++i) at.push_back(Tensor(PyList_GET_ITEM(o, i), need, 0).at);
+    return at;
+}
+
+PyObject* copy_blocks(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+    return guarded<8>(n, [&] {
+        const Shape sh(a[6]);
+        const std::vector<void*> k = layers(a[0], sh.cache), v = layers(a[1], sh.cache), ks = layers(a[2], sh.scale), vs = layers(a[3], sh.scale);
+        if (k.size() > 1 << 20 || v.size() != k.size()) throw Decline();
+        for (const auto* scales : {&ks, &vs})
+            if (scales->size() != k.size() && (sh.scaled || !scales->empty())) throw Decline();
+        const Indices copies(a[4]);
+        int32_t* count = (int32_t*)(a[5] == Py_None ? nullptr : Tensor(a[5], 4, c10::kInt).at);
+        void* s = stream_of(a[7]);
+        return unlocked([&] {
+            return lib.copy_blocks(k.data(), v.data(), ks.empty() ? nullptr : (float* const*)ks.data(), vs.empty() ? nullptr : (float* const*)vs.data(),
+                                   (int32_t)k.size(), copies.as<int32_t>(), copies.n / 2, count, &sh, s);
+        });
+    });
+}
+
 // bind(addresses of the library's functions in the order of `lib`, Shape, DecodePlan, current device, raw stream)
 PyObject* bind(PyObject*, PyObject* args)
 {
-    unsigned long long f[13];
-    PyObject* o[4];
-    if (!PyArg_ParseTuple(args, "(KKKKKKKKKKKKK)OOOO", f, f + 1, f + 2, f + 3, f + 4, f + 5, f + 6, f + 7, f + 8, f + 9,
-                          f + 10, f + 11, f + 12, o, o + 1, o + 2, o + 3))
-        return nullptr;
+    PyObject *f, *o[4];
+    if (!PyArg_ParseTuple(args, "O!OOOO", &PyTuple_Type, &f, o, o + 1, o + 2, o + 3)) return nullptr;
     void* const at[] = {&lib.write_fp8, &lib.write_fp16, &lib.decode, &lib.step, &lib.prepare, &lib.scheduled, &lib.partitioned,
-                        &lib.reduce, &lib.prefill_ws, &lib.gather, &lib.workspace_bytes, &lib.schedule_bytes, &lib.prefill_bytes};
-    for (int i = 0; i < 13; ++i) {
-        const uintptr_t p = (uintptr_t)f[i];
-        memcpy(at[i], &p, sizeof p);
+                        &lib.reduce, &lib.prefill_ws, &lib.gather, &lib.workspace_bytes, &lib.schedule_bytes, &lib.prefill_bytes,
+                        &lib.window, &lib.window_step, &lib.window_prefill, &lib.window_bytes, &lib.window_prefill_bytes, &lib.reserve,
+                        &lib.fork, &lib.free_seqs, &lib.free_window, &lib.compact, &lib.copy_blocks, &lib.blocks_bytes};
+    constexpr Py_ssize_t kFunctions = sizeof at / sizeof *at;
+    uintptr_t address[kFunctions];
+    if (PyTuple_GET_SIZE(f) != kFunctions) {
+        PyErr_SetString(PyExc_TypeError, "bind: another number of functions");
+        return nullptr;
     }
+    for (Py_ssize_t i = 0; i < kFunctions; ++i) {
+        address[i] = (uintptr_t)PyLong_AsVoidPtr(PyTuple_GET_ITEM(f, i));
+        if (PyErr_Occurred()) return nullptr;
+    }
+    for (Py_ssize_t i = 0; i < kFunctions; ++i) memcpy(at[i], address + i, sizeof *address);
     PyObject** const kept[] = {&lib.shape_class, &lib.plan_class, &lib.current_device, &lib.raw_stream};
     for (int i = 0; i < 4; ++i) {
         Py_INCREF(o[i]);
@@ -398,6 +608,8 @@ PyObject* bind(PyObject*, PyObject* args)
 #define FAST(name) {#name, (PyCFunction)(void*)name, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {FAST(write_fp8), FAST(write_fp16), FAST(decode), FAST(step), FAST(prepare), FAST(scheduled),
                          FAST(partitioned), FAST(reduce), FAST(prefill_ws), FAST(gather),
+                         FAST(window), FAST(window_step), FAST(window_prefill), FAST(reserve), FAST(fork_blocks),
+                         FAST(free_seqs), FAST(free_window), FAST(compact), FAST(copy_blocks),
                          {"bind", bind, METH_VARARGS, nullptr}, {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_binding", nullptr, -1, methods};
 
