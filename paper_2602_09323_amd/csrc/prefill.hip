@@ -932,6 +932,12 @@ extern "C" size_t coopt_prefill_workspace_bytes(const coopt_shape* sh, int32_t m
     return PrefillLaunchPlan(sh, max_chunk_len, true).workspace_bytes(sh);
 }
 
+// The tokens that a row sees at most through a window.
+static long long window_stream_tokens(const coopt_shape* sh, const Window& w)
+{
+    return std::min((long long)sh->max_blocks_per_seq * kBlock, (long long)w.size + w.sinks);
+}
+
 static int prefill_chunk(const void* q, const void* k_cache, const void* v_cache, const float* k_scale,
                          const float* v_scale, const int32_t* block_tables, const int32_t* context_lens,
                          const int32_t* query_start, int32_t num_query_rows, int32_t max_chunk_len,
@@ -952,26 +958,12 @@ extern "C" int coopt_paged_gqa_prefill_chunk(const void* q, const void* k_cache,
 
 // ---- through a sliding window (window.hpp): the same launches, planned for streams as long as a window and the sinks
 
-// What a row sees at most.
-static long long window_stream_tokens(const coopt_shape* sh, const Window& w)
-{
-    return std::min((long long)sh->max_blocks_per_seq * kBlock, (long long)w.size + w.sinks);
-}
-
-static size_t window_workspace_bytes(const coopt_shape* sh, int max_chunk_len, const Window& w)
-{
-    const PrefillLaunchPlan lp(sh, max_chunk_len, true);
-    PrefillDeal deal{};
-    deal.set(lp, sh->num_seqs * sh->num_kv_heads, window_stream_tokens(sh, w));
-    return deal.split < 2 ? 0 : lp.workspace_bytes(sh);
-}
-
 extern "C" size_t coopt_prefill_window_workspace_bytes(const coopt_shape* sh, int32_t max_chunk_len, int32_t window,
                                                        int32_t num_sinks)
 {
     if (check_shape(sh) != COOPT_OK || check_window(window, num_sinks) != COOPT_OK || max_chunk_len <= 0 || sh->num_seqs == 0)
         return 0;
-    return window_workspace_bytes(sh, max_chunk_len, window_of(sh, window, num_sinks));
+    return PrefillLaunchPlan(sh, max_chunk_len, true, window_stream_tokens(sh, window_of(sh, window, num_sinks))).workspace_bytes(sh);
 }
 
 extern "C" int coopt_paged_gqa_prefill_chunk_window(const void* q, const void* k_cache, const void* v_cache, const float* k_scale,
@@ -987,7 +979,7 @@ extern "C" int coopt_paged_gqa_prefill_chunk_window(const void* q, const void* k
     if (st != COOPT_OK) return st;
     const Window w = window_of(sh, window, num_sinks);
     if (max_chunk_len > 0 && num_query_rows > 0 && sh->num_seqs > 0) {
-        const size_t need = window_workspace_bytes(sh, max_chunk_len, w);
+        const size_t need = coopt_prefill_window_workspace_bytes(sh, max_chunk_len, window, num_sinks);
         if (need > 0 && !workspace) return COOPT_ERR_NULL;
         if (workspace_bytes < need || (need > 0 && ((uintptr_t)workspace & 15u) != 0)) return COOPT_ERR_WORKSPACE;
         if (need == 0) workspace = nullptr;
@@ -1062,10 +1054,11 @@ static int prefill_chunk(const void* q, const void* k_cache, const void* v_cache
     a.pool_tiles = sh->num_blocks * sh->num_kv_heads;
     a.scale_log2e = sh->softmax_scale * kLog2e;
 
-    const PrefillLaunchPlan lp(sh, max_chunk_len, workspace != nullptr);
-    const int pairs8 = lp.pairs8, a_per_pair = lp.a_per_pair, b_per_pair = lp.b_per_pair;
     const long long most_tokens = window ? window_stream_tokens(sh, *window) : (long long)sh->max_blocks_per_seq * kBlock;
-    a.set(lp, sh->num_seqs * sh->num_kv_heads, most_tokens);
+    const PrefillLaunchPlan lp(sh, max_chunk_len, workspace != nullptr, window ? most_tokens : 0);
+    const int pairs8 = lp.pairs8, a_per_pair = lp.a_per_pair, b_per_pair = lp.b_per_pair;
+    // (through a window the plan has weighed whole streams against parts)
+    a.set(lp, sh->num_seqs * sh->num_kv_heads, window ? 0x7fffffff : most_tokens);
     if (window) a.window = *window;
     a.part = (float*)workspace;
     const bool split = a.split >= 2;                  // (the table may hold no sequence long enough)

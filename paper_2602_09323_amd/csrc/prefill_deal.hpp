@@ -60,7 +60,10 @@ struct PrefillLaunchPlan {
     int tiles, pairs8, a_per_pair, b_per_pair, rest, parts;
     int nr;          // tiles per 64 lanes of the full-size workgroups: 2, or 1 where a pair has at most 8 tiles
     int wg_tiles;    // = 8 nr
-    PrefillLaunchPlan(const coopt_shape* sh, int max_chunk_len, bool with_workspace)
+    // window: the tokens that a row sees at most, where that is known (0: not).  A workgroup's stream is then so long
+    // and its rows longer, and its parts are counted with the ends that a part has of its own (2.3 stages, see
+    // PrefillDeal::set), the merge (about one) and the partial rows on their way to memory and back (18 MB a stage).
+    PrefillLaunchPlan(const coopt_shape* sh, int max_chunk_len, bool with_workspace, long long window = 0)
     {
         const int G = sh->num_q_heads / sh->num_kv_heads;
         tiles = G * ((max_chunk_len + 15) / 16);
@@ -83,9 +86,11 @@ struct PrefillLaunchPlan {
         // round on top (its start, its partial rows, its share of the merge)
         const long long last = (long long)pairs8 * ((r + wg_tiles - 1) / wg_tiles);
         int best = 1;
-        double best_cost = rounds(last);
+        const double stages = (double)(window + (wg_tiles + G - 1) / G * 16) / kPrefillStageTokens;
+        const double partial = 2.0 * sh->num_seqs * sh->num_kv_heads * r * 16 * (sh->head_dim + 2) * 4 / 18e6;
+        double best_cost = window > 0 ? rounds(last) * (2.3 + stages) : rounds(last);
         for (int p = 2; p <= kPrefillMaxParts; ++p) {
-            const double cost = rounds(last * p) / p + 0.02 * (p - 1);
+            const double cost = window > 0 ? rounds(last * p) * (2.3 + stages / p) + 1.0 + p * partial : rounds(last * p) / p + 0.02 * (p - 1);
             if (cost < best_cost) {
                 best_cost = cost;
                 best = p;
@@ -97,7 +102,7 @@ struct PrefillLaunchPlan {
             parts = best;
             return;
         }
-        if (cand >= 1 && nr == 2) {
+        if (cand >= 1 && nr == 2 && window == 0) {
             const int small = (r + kPrefillWaves - 1) / kPrefillWaves;
             const double split = rounds((long long)pairs8 * cand) + 0.65 * rounds((long long)pairs8 * small);
             if (split < rounds(W)) {
@@ -110,7 +115,7 @@ struct PrefillLaunchPlan {
         // What a workspace would split runs whole, but behind the same cut: which rows share a wavefront
         // decides when their references are raised, and the tiles in front of the cut are to have the
         // same bits with and without a workspace.
-        if (best >= 2) {
+        if (best >= 2 && window == 0) {
             a_per_pair = cand;
             rest = r;
             parts = 1;
