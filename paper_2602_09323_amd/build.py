@@ -22,13 +22,14 @@ CSRC = os.path.join(HERE, "csrc")
 BUILD = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libcoopt_attn.so")
 PROBE_LIB = os.path.join(HERE, "libcoopt_probe.so")      # measurement aid, not the product
-SOURCES = ["kv_write.hip", "decode.hip", "decode_flat.hip", "prefill.hip", "gather.hip", "blocks.hip"]
+SOURCES = ["kv_write.hip", "decode.hip", "decode_flat.hip", "prefill.hip", "gather.hip", "blocks.hip", "window_tile.hip"]
 PROBE_SOURCES = ["probe.hip"]
 BINDING = os.path.join(HERE, "_binding" + (sysconfig.get_config_var("EXT_SUFFIX") or ".so"))
 BINDING_SOURCE = "binding_native.cpp"                    # host code: tensors to pointers, no kernel
 BINDING_STAMP = os.path.join(HERE, "_binding.built_for")   # the torch that it was last compiled against, or did not compile
 HEADERS = [os.path.join(CSRC, h) for h in ("common.hpp", "attn_tile.hpp", "kv_quant.hpp",
-                                          "decode_internal.hpp", "launch_grid.hpp", "prefill_deal.hpp", "window.hpp")] + [
+                                          "decode_internal.hpp", "launch_grid.hpp", "prefill_deal.hpp", "window.hpp",
+                                          "window_tile.hpp")] + [
     os.path.join(ROOT, "include", "coopt_attn.h"), os.path.join(ROOT, "include", "coopt_probe.h")]
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-fno-gpu-rdc",
          "-I" + os.path.join(ROOT, "include"),

@@ -1182,7 +1182,7 @@ pair_decode_kernel(const FlatArgs a)
         t = v.t;
         hole_lo = v.lo;
         hole_hi = v.hi;
-        if (my_block * kBlock < t) ids = bt[v.block(my_block)];
+        if (my_block * kBlock < t && v.block(my_block) < a.max_blocks) ids = bt[v.block(my_block)];
     }
     const int nb = (t + kBlock - 1) / kBlock, ng = (nb + 1) >> 1;
     const int first = part * kWaves + wave;

@@ -47,15 +47,19 @@
 // workgroup 6-8 us after the stream's end, so 3), the block numbers of three stages are asked for
 // before anything else, and nothing is read ahead of the stream (a pass over all v_scales for their
 // largest took 3-6 us a workgroup).  Together: the three prompts 102 -> 90 us, 8 x 352 rows 92 -> 80.
-#include <algorithm>
-
 #include "attn_tile.hpp"
 #include "kv_quant.hpp"
 #include "launch_grid.hpp"
 #include "prefill_deal.hpp"
 #include "window.hpp"
+#include "window_tile.hpp"
 
 namespace coopt {
+
+// window_tile.hip: one tile a workgroup.
+int launch_window_tiles(const void* q, const void* k_cache, const void* v_cache, const float* k_scale, const float* v_scale,
+                        const int32_t* block_tables, const int32_t* context_lens, const int32_t* query_start, int max_chunk_len,
+                        const Window& window, void* out, const coopt_shape* sh, int waves, hipStream_t stream);
 
 struct PrefillArgs : PrefillDeal {
     const half_t* q;
@@ -932,12 +936,6 @@ extern "C" size_t coopt_prefill_workspace_bytes(const coopt_shape* sh, int32_t m
     return PrefillLaunchPlan(sh, max_chunk_len, true).workspace_bytes(sh);
 }
 
-// The tokens that a row sees at most through a window.
-static long long window_stream_tokens(const coopt_shape* sh, const Window& w)
-{
-    return std::min((long long)sh->max_blocks_per_seq * kBlock, (long long)w.size + w.sinks);
-}
-
 static int prefill_chunk(const void* q, const void* k_cache, const void* v_cache, const float* k_scale,
                          const float* v_scale, const int32_t* block_tables, const int32_t* context_lens,
                          const int32_t* query_start, int32_t num_query_rows, int32_t max_chunk_len,
@@ -963,7 +961,9 @@ extern "C" size_t coopt_prefill_window_workspace_bytes(const coopt_shape* sh, in
 {
     if (check_shape(sh) != COOPT_OK || check_window(window, num_sinks) != COOPT_OK || max_chunk_len <= 0 || sh->num_seqs == 0)
         return 0;
-    return PrefillLaunchPlan(sh, max_chunk_len, true, window_stream_tokens(sh, window_of(sh, window, num_sinks))).workspace_bytes(sh);
+    const Window w = window_of(sh, window, num_sinks);
+    if (window_tile_waves(sh, max_chunk_len, w) > 0) return 0;
+    return PrefillLaunchPlan(sh, max_chunk_len, true, window_row_tokens(sh, w)).workspace_bytes(sh);
 }
 
 extern "C" int coopt_paged_gqa_prefill_chunk_window(const void* q, const void* k_cache, const void* v_cache, const float* k_scale,
@@ -1038,6 +1038,12 @@ static int prefill_chunk(const void* q, const void* k_cache, const void* v_cache
     if (!q || !k_cache || !v_cache || !block_tables || !context_lens || !query_start || !out)
         return COOPT_ERR_NULL;
     if (sh->kv_dtype != COOPT_KV_FP16 && (!k_scale || !v_scale)) return COOPT_ERR_NULL;
+    if (window) {
+        const int waves = window_tile_waves(sh, max_chunk_len, *window);
+        if (waves > 0)
+            return launch_window_tiles(q, k_cache, v_cache, k_scale, v_scale, block_tables, context_lens, query_start, max_chunk_len,
+                                       *window, out, sh, waves, (hipStream_t)hip_stream);
+    }
 
     PrefillArgs a{};
     a.q = (const half_t*)q;
@@ -1054,7 +1060,7 @@ static int prefill_chunk(const void* q, const void* k_cache, const void* v_cache
     a.pool_tiles = sh->num_blocks * sh->num_kv_heads;
     a.scale_log2e = sh->softmax_scale * kLog2e;
 
-    const long long most_tokens = window ? window_stream_tokens(sh, *window) : (long long)sh->max_blocks_per_seq * kBlock;
+    const long long most_tokens = window ? window_row_tokens(sh, *window) : (long long)sh->max_blocks_per_seq * kBlock;
     const PrefillLaunchPlan lp(sh, max_chunk_len, workspace != nullptr, window ? most_tokens : 0);
     const int pairs8 = lp.pairs8, a_per_pair = lp.a_per_pair, b_per_pair = lp.b_per_pair;
     // (through a window the plan has weighed whole streams against parts)

@@ -60,6 +60,7 @@ struct PrefillLaunchPlan {
     int tiles, pairs8, a_per_pair, b_per_pair, rest, parts;
     int nr;          // tiles per 64 lanes of the full-size workgroups: 2, or 1 where a pair has at most 8 tiles
     int wg_tiles;    // = 8 nr
+    double cost;     // of the plan, in stages, where window is given
     // window: the tokens that a row sees at most, where that is known (0: not).  A workgroup's stream is then so long
     // and its rows longer, and its parts are counted with the ends that a part has of its own (2.3 stages, see
     // PrefillDeal::set), the merge (about one) and the partial rows on their way to memory and back (18 MB a stage).
@@ -80,13 +81,14 @@ struct PrefillLaunchPlan {
         auto rounds = [](long long wgs) { return (double)((wgs + kPrefillCUs - 1) / kPrefillCUs); };
         const long long W = (long long)pairs8 * full_per_pair;
         const int cand = (int)((W / kPrefillCUs) * kPrefillCUs / pairs8);   // full rounds only
+        const double stages = (double)(window + (wg_tiles + G - 1) / G * 16) / kPrefillStageTokens;
+        cost = rounds((long long)pairs8 * cand) * (2.3 + stages);
         if (cand >= full_per_pair) return;                                   // whole rounds
         const int r = tiles - cand * wg_tiles;                               // tiles of the last round, per pair
         // p parts make p times the workgroups, each 1/p as long; a part costs about 2 % of a
         // round on top (its start, its partial rows, its share of the merge)
         const long long last = (long long)pairs8 * ((r + wg_tiles - 1) / wg_tiles);
         int best = 1;
-        const double stages = (double)(window + (wg_tiles + G - 1) / G * 16) / kPrefillStageTokens;
         const double partial = 2.0 * sh->num_seqs * sh->num_kv_heads * r * 16 * (sh->head_dim + 2) * 4 / 18e6;
         double best_cost = window > 0 ? rounds(last) * (2.3 + stages) : rounds(last);
         for (int p = 2; p <= kPrefillMaxParts; ++p) {
@@ -96,6 +98,7 @@ struct PrefillLaunchPlan {
                 best = p;
             }
         }
+        cost += best_cost;
         if (best >= 2 && with_workspace) {
             a_per_pair = cand;
             rest = r;

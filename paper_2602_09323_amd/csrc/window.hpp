@@ -53,6 +53,13 @@ inline Window window_of(const coopt_shape* sh, int window, int num_sinks)
     return Window{window < most ? window : most, num_sinks < most ? num_sinks : most};
 }
 
+// The tokens that a row sees at most.
+inline long long window_row_tokens(const coopt_shape* sh, const Window& w)
+{
+    const long long most = (long long)sh->max_blocks_per_seq * sh->block_size, seen = (long long)w.size + w.sinks;
+    return seen < most ? seen : most;
+}
+
 // The shape with a table as wide as the most blocks that a view over `rows` neighbouring tokens' windows has.
 inline coopt_shape window_shape(const coopt_shape* sh, const Window& w, int rows = 1)
 {

@@ -65,7 +65,7 @@ def test_decode(oracle_mod, kv, H_q, H_k, d, window, sinks):
 
 
 @pytest.mark.parametrize("lens,window,sinks", [([2500, 1], 2048, 4), ([9000, 4097, 130, 3], 4096, 13),
-                                               ([1200] * 70 + [5] * 3, 512, 4), ([6000], 512, 4), ([300] * 150, 128, 0)])
+                                               ([620] * 70 + [5] * 3, 512, 4), ([6000], 512, 4), ([150] * 150, 128, 0)])
 @pytest.mark.parametrize("kv,H_q,H_k,d", [("e4m3", 40, 8, 128), ("fp16", 8, 8, 64)])
 def test_decode_of_longer_contexts(oracle_mod, kv, H_q, H_k, d, lens, window, sinks):
     """Batches and contexts large enough for every way of cutting the work."""
@@ -76,7 +76,7 @@ def test_decode_of_longer_contexts(oracle_mod, kv, H_q, H_k, d, lens, window, si
 
 
 @pytest.mark.parametrize("lens,window,sinks", [(LENS, 1, 0), (LENS, 17, 4), (LENS, 333, 33), ([2500, 1, 0, 700], 2048, 4),
-                                               ([1200] * 70 + [5] * 3, 512, 4)])
+                                               ([620] * 70 + [5] * 3, 512, 4)])
 @pytest.mark.parametrize("kv,H_q,H_k,d", HEADS)
 def test_fused_step(oracle_mod, kv, H_q, H_k, d, lens, window, sinks):
     """The write of the new tokens and the attention in one call: every third sequence's slot is negative (nothing
@@ -146,6 +146,24 @@ def test_prefill_of_longer_chunks(oracle_mod, kv, H_q, H_k, d, chunks, lens, win
     cache, tables = poisoned(oracle_mod, w, hidden_from(w, chunks, window, sinks))
     ref = window_attention(w, cache, q, w.context_lens, starts, window, sinks)
     assert_close(hip_prefill_window(w, cache_to_dev(cache), tables, q, starts, window, sinks), ref, f"{chunks} window {window}")
+
+
+# (chunks, lengths, window, sinks) that between them reach every form of the launch, for every cache and head size: the
+# number of wavefronts a tile, whole streams, streams in parts, short chunks (test_window_view.py asks the rule)
+FORM_HEADS = [("e4m3", 40, 8, 128), ("e4m3", 32, 8, 64), ("e5m2", 40, 8, 128), ("e5m2", 32, 8, 64), ("fp16", 16, 8, 128), ("fp16", 32, 8, 64)]
+FORM_CASES = [([30, 7], [800, 90], 130, 4), ([16], [700], 500, 4), ([16], [2500], 2400, 4), ([16, 16], [4300, 60], 4000, 7),
+              ([40] * 10 + [5], [40] * 10 + [5], 16, 0), ([1500, 40], [3500, 2500], 900, 20), ([700], [5000], 4100, 4),
+              ([500] * 5, [500] * 5, 33, 4)]
+
+
+@pytest.mark.parametrize("chunks,lens,window,sinks", FORM_CASES)
+@pytest.mark.parametrize("kv,H_q,H_k,d", FORM_HEADS)
+def test_prefill_in_every_form(oracle_mod, kv, H_q, H_k, d, chunks, lens, window, sinks):
+    w = random_workload("window_forms", 22, kv, H_q, H_k, d, lens)
+    q, starts = ragged_rows(w, chunks)
+    cache, tables = poisoned(oracle_mod, w, hidden_from(w, chunks, window, sinks))
+    ref = window_attention(w, cache, q, w.context_lens, starts, window, sinks)
+    assert_close(hip_prefill_window(w, cache_to_dev(cache), tables, q, starts, window, sinks), ref, f"{chunks[:3]} window {window}")
 
 
 @pytest.mark.parametrize("kv,H_q,H_k,d", HEADS[:2])

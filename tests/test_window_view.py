@@ -76,6 +76,87 @@ def test_views(tmp_path):
     assert subprocess.run([str(exe)], check=True, capture_output=True, text=True).stdout == ""
 
 
+TILES = r"""
+#include <cstdio>
+#include <initializer_list>
+#define __device__
+#define __forceinline__ inline
+using std::max;
+using std::min;
+template <class T> T wave_uniform(T v) { return v; }
+#include "window_tile.hpp"
+using namespace coopt;
+int main()
+{
+    // every wavefront's blocks fit its lanes, whatever the rule says, and the workspace is asked for by the same rule
+    for (int kv : {0, 1, 2})
+        for (int d : {64, 128})
+            for (int hk : {1, 2, 7, 8, 40})
+                for (int g : {1, 5, 16})
+                    for (int seqs : {1, 3, 64, 1 << 16})
+                        for (int chunk : {1, 16, 77, 2000})
+                            for (int window : {1, 16, 100, 1024, 5000, 1 << 28})
+                                for (int sinks : {0, 4, 5000})
+                                    for (int width : {1, 70, 1 << 20}) {
+                                        const coopt_shape sh = {seqs, hk * g, hk, d, 16, 1, width, kv, 1.0f};
+                                        const Window w = window_of(&sh, window, sinks);
+                                        const int waves = window_tile_waves(&sh, chunk, w);
+                                        const int groups = (window_shape(&sh, w, 16).max_blocks_per_seq + 1) / 2;
+                                        if (waves < 0 || waves > 4 || (waves & (waves - 1))) printf("%d wavefronts\n", waves);
+                                        if (waves && (groups + waves - 1) / waves > kWindowTileGroups) printf("%d groups for %d\n", groups, waves);
+                                    }
+    return 0;
+}
+"""
+
+# what the cases of test_gpu_window.py reach: (kv, q heads, kv heads, dim, sequences, longest chunk, table, window, sinks)
+FORMS = r"""
+int main()
+{
+    int a[9];
+    while (scanf("%d %d %d %d %d %d %d %d %d", a, a + 1, a + 2, a + 3, a + 4, a + 5, a + 6, a + 7, a + 8) == 9) {
+        const coopt_shape sh = {a[4], a[1], a[2], a[3], 16, 1, a[6], a[0], 1.0f};
+        const Window w = window_of(&sh, a[7], a[8]);
+        const int waves = window_tile_waves(&sh, a[5], w);
+        const PrefillLaunchPlan plan(&sh, a[5], true, window_row_tokens(&sh, w));
+        if (waves) printf("tile%d\n", waves);
+        else printf("stream%d%s\n", plan.wg_tiles, plan.parts > 1 ? "parts" : "");
+    }
+    return 0;
+}
+"""
+
+
+def _program(tmp_path, source, name):
+    src, exe = tmp_path / f"{name}.cpp", tmp_path / name
+    src.write_text("#include <algorithm>\n" + source)
+    subprocess.run(["g++", "-std=c++17", "-O1", f"-I{ROOT / 'paper_2602_09323_amd' / 'csrc'}", f"-I{ROOT / 'include'}",
+                    str(src), "-o", str(exe)], check=True)
+    return str(exe)
+
+
+def test_the_rule_of_the_tiles(tmp_path):
+    assert subprocess.run([_program(tmp_path, TILES, "tiles")], check=True, capture_output=True, text=True).stdout == ""
+
+
+def test_every_form_has_its_cases(tmp_path):
+    import test_gpu_window as cases
+    program = _program(tmp_path, TILES[:TILES.index("int main")] + FORMS, "forms")
+    kinds = {"fp16": 0, "e4m3": 1, "e5m2": 2}
+    lines = []
+    for kv, H_q, H_k, d in cases.FORM_HEADS:
+        for chunks, lens, window, sinks in cases.FORM_CASES:
+            lines.append((kinds[kv], H_q, H_k, d, len(lens), max(chunks), -(-max(lens) // 16), window, sinks))
+    said = subprocess.run([program], input="\n".join(" ".join(map(str, x)) for x in lines), check=True, capture_output=True,
+                          text=True).stdout.split()
+    for kv in range(3):
+        for d in (64, 128):
+            found = {s for s, x in zip(said, lines) if x[0] == kv and x[3] == d}
+            assert {"tile1", "tile2", "tile4"} <= found, (kv, d, found)
+            assert {x[:8] for x in found} >= {"stream16"} and {x[:7] for x in found} >= {"stream8"}, (kv, d, found)
+    assert {"stream16", "stream16parts", "stream8parts"} <= set(said)
+
+
 def test_refusals(lib):  # noqa: F811
     """Before any launch: nothing is read through these pointers."""
     one, size = ctypes.c_void_p(16), ctypes.c_size_t

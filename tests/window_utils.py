@@ -4,33 +4,35 @@ import numpy as np
 import torch
 
 import workloads
-from helpers import k_logical, k_store_logical, oracle_fill, v_logical, v_store_logical
+from helpers import k_tile_index, oracle_fill, v_tile_index
 
 
-def _values(w):
-    """The value of every code, or None for an fp16 cache."""
-    if w.kv_dtype == "fp16":
-        return None
-    code = torch.float8_e4m3fn if w.kv_dtype == "e4m3" else torch.float8_e5m2
-    return torch.arange(256, dtype=torch.uint8).view(code).to(torch.float64).numpy()
+CODES = {"e4m3": torch.float8_e4m3fn, "e5m2": torch.float8_e5m2}
 
 
-def rows_of(w, cache, s, keys):
-    """K and V [len(keys), H_k, d] float64 of sequence s's tokens `keys`."""
-    block, place = w.block_tables[s, keys // w.B], keys % w.B
-    table = _values(w)
-    out = []
-    for logical, data, scale in ((k_logical, cache[0], cache[2]), (v_logical, cache[1], cache[3])):
-        x = logical(_Part(w, len(block)), data[block])[np.arange(len(block)), :, place]
-        out.append(x.astype(np.float64) if table is None
-                   else table[x] * scale[block, :, place].astype(np.float64)[:, :, None])
-    return out
+class Rows:
+    """K and V [H_k, keys, d] in 64 bits of a sequence's tokens, from the cache's bytes."""
+    def __init__(self, w, cache):
+        self.w = w
+        self.where = "cuda" if torch.cuda.is_available() else "cpu"
+        self.cache = [None if x is None else torch.from_numpy(x).to(self.where) for x in cache]
+        E = 8 if w.kv_dtype == "fp16" else 16
+        self.places = [torch.from_numpy(f(w.d, E, w.B)).to(self.where) for f in (k_tile_index, v_tile_index)]
 
-
-class _Part:
-    """The workload's tile layout over a pool of n blocks."""
-    def __init__(self, w, n):
-        self.NB, self.H_k, self.B, self.d, self.kv_dtype = n, w.H_k, w.B, w.d, w.kv_dtype
+    def of(self, s, keys):
+        w = self.w
+        block = torch.from_numpy(w.block_tables[s, keys // w.B].astype(np.int64)).to(self.where)
+        place = torch.from_numpy(keys % w.B).to(self.where)
+        out = []
+        for data, scale, at in ((self.cache[0], self.cache[2], self.places[0]), (self.cache[1], self.cache[3], self.places[1])):
+            x = data[block].gather(2, at[place][:, None].expand(-1, w.H_k, -1))
+            if scale is None:
+                x = x.double()
+            else:
+                one = scale[block].gather(2, place[:, None, None].expand(-1, w.H_k, 1))
+                x = x.view(CODES[w.kv_dtype]).double() * one.double()
+            out.append(x.permute(1, 0, 2).contiguous())
+        return out
 
 
 def seen_keys(p, window, sinks):
@@ -41,8 +43,9 @@ def seen_keys(p, window, sinks):
 
 def window_attention(w, cache, q, lens, starts, window, sinks):
     """[rows, H_q, d] float64: sequence s's rows starts[s] .. starts[s+1]-1 are its last tokens."""
-    G, where = w.H_q // w.H_k, "cuda" if torch.cuda.is_available() else "cpu"
-    out = np.zeros(q.shape)
+    G, rows = w.H_q // w.H_k, Rows(w, cache)
+    where = rows.where
+    out = torch.zeros(q.shape, dtype=torch.float64, device=where)
     for s in range(len(lens)):
         C = int(starts[s + 1] - starts[s])
         t = int(lens[s])
@@ -50,17 +53,17 @@ def window_attention(w, cache, q, lens, starts, window, sinks):
             continue
         first = max(t - C + 1 - window, 0)                 # of the first row's window
         keys = np.union1d(np.arange(min(sinks, t)), np.arange(first, t))
-        K, V = (torch.from_numpy(x.transpose(1, 0, 2).copy()).to(where) for x in rows_of(w, cache, s, keys))
-        x = q[starts[s]:starts[s + 1]].astype(np.float64).reshape(C, w.H_k, G, w.d).transpose(1, 2, 0, 3)
-        x = torch.from_numpy(x.reshape(w.H_k, G * C, w.d).copy()).to(where)
+        K, V = rows.of(s, keys)
+        x = torch.from_numpy(q[starts[s]:starts[s + 1]]).to(where).double().view(C, w.H_k, G, w.d)
+        x = x.permute(1, 2, 0, 3).reshape(w.H_k, G * C, w.d)
         p = np.arange(t - C, t)[:, None]
         seen = torch.from_numpy((keys <= p) & ((keys > p - window) | (keys < sinks))).to(where)
         for g in range(w.H_k):
             z = torch.matmul(x[g], K[g].T.contiguous()).view(G, C, -1) * w.softmax_scale
             z = torch.softmax(z.masked_fill(~seen, -np.inf), -1).view(G * C, -1)
             o = torch.matmul(z, V[g]).view(G, C, w.d)
-            out[starts[s]:starts[s + 1], g * G:(g + 1) * G] = o.permute(1, 0, 2).cpu().numpy()
-    return out
+            out[starts[s]:starts[s + 1], g * G:(g + 1) * G] = o.permute(1, 0, 2)
+    return out.cpu().numpy()
 
 
 def poisoned(oracle, w, hidden):
@@ -71,24 +74,27 @@ def poisoned(oracle, w, hidden):
     nan = {"e4m3": 0x7F, "e5m2": 0x7F, "fp16": np.float16(np.nan)}[w.kv_dtype]
     bad = w.NB - 1
     assert bad not in w.block_tables
-    kl, vl = k_logical(w, cache[0]), v_logical(w, cache[1])
-    kl[bad] = vl[bad] = nan
-    if cache[2] is not None:
-        cache[2][bad] = cache[3][bad] = np.nan
+    for x, value in zip(cache, (nan, nan, np.nan, np.nan)):
+        if x is not None:
+            x[bad] = value
     tables = w.block_tables.copy()
+    blocks, places = [], []
     for s in range(w.S):
         t = int(w.context_lens[s])
         gone = np.zeros(w.max_blocks * w.B, bool)
         gone[t:] = True
         gone[hidden(s)] = True
-        for j in np.flatnonzero(gone[:t]):
-            b, place = tables[s, j // w.B], j % w.B
-            kl[b, :, place] = vl[b, :, place] = nan
-            if cache[2] is not None:
-                cache[2][b, :, place] = cache[3][b, :, place] = np.nan
+        j = np.flatnonzero(gone[:t])
+        blocks.append(tables[s, j // w.B])
+        places.append(j % w.B)
         tables[s][gone.reshape(-1, w.B).all(axis=1)] = bad
-    k_store_logical(w, cache[0], kl)
-    v_store_logical(w, cache[1], vl)
+    blocks, places = np.concatenate(blocks), np.concatenate(places)
+    heads, E = np.arange(w.H_k)[:, None], 8 if w.kv_dtype == "fp16" else 16
+    for x, f in ((cache[0], k_tile_index), (cache[1], v_tile_index)):
+        x[blocks[:, None, None], heads, f(w.d, E, w.B)[places][:, None]] = nan
+    for x in cache[2:]:
+        if x is not None:
+            x[blocks, :, places] = np.nan
     return cache, tables
 
 
