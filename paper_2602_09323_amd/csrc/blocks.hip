@@ -18,7 +18,9 @@ namespace coopt {
 
 constexpr int kPlanThreads = 1024;             // of the workgroup that plans
 constexpr int kPlanWaves = kPlanThreads / 64;
-constexpr int kListed = 4096;                  // new blocks kept in LDS; more go to the workspace
+constexpr int kListed = 8192;                  // new blocks kept in LDS; more go to the workspace
+constexpr long long kFewEntries = 8192;        // table entries that the planning workgroup works on itself: a second launch
+                                               // takes longer (8 forks of 44 entries: 5.7 + 3.6 us, 6.0 so)
 
 // Where a call's parts lie in the workspace (32-bit words).
 struct BlocksWorkspace {
@@ -81,14 +83,15 @@ __device__ __forceinline__ uint32_t free_word(const BlocksArgs& a, int w)
 }
 
 // The `need` lowest free blocks, into list[0 .. need-1], and out of the map with a reference each -- or, where
-// there are fewer, nothing but how many are missing.  cut: a word of LDS.
-__device__ __forceinline__ int take_blocks(const BlocksArgs& a, int need, int* list, int* sums, int* cut)
+// there are fewer, nothing but how many are missing.  first_word: the thread's word of the map's first; cut: a
+// word of LDS.
+__device__ __forceinline__ int take_blocks(const BlocksArgs& a, uint32_t first_word, int need, int* list, int* sums, int* cut)
 {
     if (need <= 0) return 0;
     int have = 0, base = 0;
     for (; base < a.words && have < need; base += kPlanThreads) {
         const int w = base + threadIdx.x;
-        uint32_t bits = free_word(a, w);
+        uint32_t bits = base == 0 ? first_word : free_word(a, w);
         int total, at = have + plan_scan(__builtin_popcount(bits), sums, total);
         if (at < need && at + __builtin_popcount(bits) >= need) *cut = w;          // the last word that is taken from
         for (; bits && at < need; ++at, bits &= bits - 1) list[at] = 32 * w + __builtin_ctz(bits);
@@ -147,7 +150,7 @@ blocks_map_kernel(const BlocksArgs a)
 // ---- freeing
 
 // A workgroup per listed sequence: its length is taken out first, so that the same index twice frees once.
-__global__ void __launch_bounds__(256)
+__global__ void __launch_bounds__(1024)
 blocks_free_kernel(const BlocksArgs a, const int32_t* seqs)
 {
     __shared__ int tokens;
@@ -156,7 +159,7 @@ blocks_free_kernel(const BlocksArgs a, const int32_t* seqs)
     if (threadIdx.x == 0) tokens = atomicExch(a.lens + s, 0);
     __syncthreads();
     const int nb = min(blocks_of(max(tokens, 0)), a.max_blocks);
-    for (int b = threadIdx.x; b < nb; b += 256) release(a, a.tables[(size_t)s * a.max_blocks + b]);
+    for (int b = threadIdx.x; b < nb; b += blockDim.x) release(a, a.tables[(size_t)s * a.max_blocks + b]);
 }
 
 // A wavefront per sequence, from the window down: what earlier calls have freed (-1) lies below, so
@@ -200,6 +203,7 @@ blocks_reserve_kernel(const BlocksArgs a, const int32_t* starts, int num_rows, i
 {
     __shared__ int sums[kPlanWaves], cut, refused, listed[kListed], first_listed[kPlanThreads];
     if (threadIdx.x == 0) refused = starts && (starts[0] != 0 || starts[a.num_seqs] > num_rows);
+    const uint32_t word = free_word(a, threadIdx.x);        // (asked for with the lengths)
     int* first = a.num_seqs <= kPlanThreads ? first_listed : a.ws.first;
     int need = 0;
     __syncthreads();
@@ -218,7 +222,7 @@ blocks_reserve_kernel(const BlocksArgs a, const int32_t* starts, int num_rows, i
     }
     __syncthreads();
     int* list = need <= kListed ? listed : a.ws.list;
-    const int missing = refused ? -1 : take_blocks(a, need, list, sums, &cut);
+    const int missing = refused ? -1 : take_blocks(a, word, need, list, sums, &cut);
     if (threadIdx.x == 0) *result = missing;
     const int rows = starts ? min(max(starts[a.num_seqs], 0), num_rows) : a.num_seqs;
     if (missing != 0) {
@@ -262,12 +266,26 @@ blocks_slots_kernel(const BlocksArgs a, const int32_t* starts, int num_rows, int
 
 // ---- forks
 
+// The first `full` entries of a parent's row for the child as well, every step-th from `first` on.
+__device__ __forceinline__ void share_row(const BlocksArgs& a, int parent, int child, int full, int first, int step)
+{
+    const int32_t* from = a.tables + (size_t)parent * a.max_blocks;
+    int32_t* to = a.tables + (size_t)child * a.max_blocks;
+    for (int b = first; b < full; b += step) {
+        const int id = from[b];
+        to[b] = id;
+        if (is_block(a, id)) atomicAdd(a.refs + id, 1);
+    }
+}
+
 __global__ void __launch_bounds__(kPlanThreads)
-blocks_fork_kernel(const BlocksArgs a, const int32_t* parents, const int32_t* children, int n, int32_t* copies, int32_t* result)
+blocks_fork_kernel(const BlocksArgs a, const int32_t* parents, const int32_t* children, int n, int32_t* copies, int32_t* result,
+                   int shares)
 {
     __shared__ int sums[kPlanWaves], cut, refused, listed[kListed];
     if (threadIdx.x == 0) refused = 0;
     __syncthreads();
+    const uint32_t word = free_word(a, threadIdx.x);        // (asked for with the lengths)
     int* tokens = a.ws.first;
     auto is_seq = [&](int s) { return (uint32_t)s < (uint32_t)a.num_seqs; };
     // (a pair with a negative index is none)
@@ -294,7 +312,7 @@ blocks_fork_kernel(const BlocksArgs a, const int32_t* parents, const int32_t* ch
     }
     __syncthreads();
     int* list = need <= kListed ? listed : a.ws.list;
-    const int missing = refused ? -1 : take_blocks(a, need, list, sums, &cut);
+    const int missing = refused ? -1 : take_blocks(a, word, need, list, sums, &cut);
     if (threadIdx.x == 0) *result = missing;
     __syncthreads();
     int before = 0;
@@ -319,6 +337,10 @@ blocks_fork_kernel(const BlocksArgs a, const int32_t* parents, const int32_t* ch
         copies[2 * i] = src;
         copies[2 * i + 1] = dst;
     }
+    // (few children: a wavefront each, and no launch behind this one)
+    if (shares && missing == 0)
+        for (int i = threadIdx.x >> 6; i < n; i += kPlanWaves)
+            if (tokens[i] > 0) share_row(a, parents[i], children[i], tokens[i] / kBlock, threadIdx.x & 63, 64);
 }
 
 // The full blocks of a parent, shared with the child (blockIdx.y: every so many of them).
@@ -327,18 +349,26 @@ blocks_share_kernel(const BlocksArgs a, const int32_t* parents, const int32_t* c
 {
     const int p = parents[blockIdx.x], c = children[blockIdx.x];
     if (p < 0 || c < 0 || *result != 0) return;
-    const int full = a.lens[c] / kBlock;
-    for (int b = blockIdx.y * 256 + threadIdx.x; b < full; b += gridDim.y * 256) {
-        const int id = a.tables[(size_t)p * a.max_blocks + b];
-        a.tables[(size_t)c * a.max_blocks + b] = id;
-        if (is_block(a, id)) atomicAdd(a.refs + id, 1);
-    }
+    share_row(a, p, c, a.lens[c] / kBlock, blockIdx.y * 256 + threadIdx.x, gridDim.y * 256);
 }
 
 // ---- compaction: of n blocks in use, those numbered n and above move, in order, to the free ones below n
 
+// The new numbers of the blocks that sequence s holds, every step-th entry from `first` on.
+__device__ __forceinline__ void renumber_row(const BlocksArgs& a, int s, int used, int first, int step)
+{
+    const int nb = min(blocks_of(max(a.lens[s], 0)), a.max_blocks);
+    int32_t* row = a.tables + (size_t)s * a.max_blocks;
+    for (int b = first; b < nb; b += step) {
+        const int id = row[b];
+        if (!is_block(a, id) || id < used) continue;
+        const int to = a.ws.list[id];
+        if (is_block(a, to)) row[b] = to;
+    }
+}
+
 __global__ void __launch_bounds__(kPlanThreads)
-blocks_compact_kernel(const BlocksArgs a, int32_t* copies, int32_t* num_copies)
+blocks_compact_kernel(const BlocksArgs a, int32_t* copies, int32_t* num_copies, int renumbers)
 {
     __shared__ int sums[kPlanWaves];
     int used = a.num_blocks;
@@ -372,20 +402,15 @@ blocks_compact_kernel(const BlocksArgs a, int32_t* copies, int32_t* num_copies)
         *num_copies = moved;
         *a.ws.used = used;
     }
+    if (!renumbers) return;
+    __syncthreads();
+    for (int s = threadIdx.x >> 6; s < a.num_seqs; s += kPlanWaves) renumber_row(a, s, used, threadIdx.x & 63, 64);
 }
 
 __global__ void __launch_bounds__(256)
 blocks_renumber_kernel(const BlocksArgs a)
 {
-    const int used = *a.ws.used;
-    const int nb = min(blocks_of(max(a.lens[blockIdx.x], 0)), a.max_blocks);
-    int32_t* row = a.tables + (size_t)blockIdx.x * a.max_blocks;
-    for (int b = blockIdx.y * 256 + threadIdx.x; b < nb; b += gridDim.y * 256) {
-        const int id = row[b];
-        if (!is_block(a, id) || id < used) continue;
-        const int to = a.ws.list[id];
-        if (is_block(a, to)) row[b] = to;
-    }
+    renumber_row(a, blockIdx.x, *a.ws.used, blockIdx.y * 256 + threadIdx.x, gridDim.y * 256);
 }
 
 // ---- copying blocks, in all layers of a launch
@@ -401,31 +426,53 @@ struct CopyArgs {
     const int32_t* num_copies;      // NULL: max_copies
     int32_t max_copies, num_blocks, layers;
     uint32_t kv_bytes, scale_bytes; // of a block in one layer
+    uint32_t pieces;                // of a block's K and V
     CopyLayer layer[kCopyLayers];
 };
 
 typedef uint32_t copy_t __attribute__((ext_vector_type(4), aligned(4)));
 
-// A workgroup per block and layer in turn.
+constexpr uint32_t kCopyPiece = 16384;         // bytes a workgroup has in flight: 4 loads of 16 a thread
+
+// A piece of a block's K and V in one layer at a time, the scales with the first; all of a piece's loads are asked for
+// before its first store.  Bound by HBM where there are enough pieces to fill the chip: 4.85 GB (both ways) of a
+// compaction in 16 layers 960 us, 5.05 TB/s; one block of 8 samples in 40 layers, 21.6 MB, 6.2 us.  (A workgroup per block
+// and layer that copied K, then V, 4 KB at a time: 1017 us and 7.1.)
 __global__ void __launch_bounds__(256)
 blocks_copy_kernel(const CopyArgs a)
 {
-    const int n = a.num_copies ? min(*a.num_copies, a.max_copies) : a.max_copies;
-    for (long long i = blockIdx.x; i < (long long)n * a.layers; i += gridDim.x) {
-        const int layer = (int)(i / n), pair = (int)(i - (long long)layer * n);
+    const uint32_t n = a.num_copies ? (uint32_t)min(max(*a.num_copies, 0), a.max_copies) : (uint32_t)a.max_copies;
+    const uint32_t per_layer = n * a.pieces;                // (the host has seen that it fits)
+    for (uint32_t layer = 0, i = blockIdx.x; layer < (uint32_t)a.layers;) {
+        if (i >= per_layer) {
+            i -= per_layer;
+            ++layer;
+            continue;
+        }
+        const uint32_t pair = i / a.pieces, piece = i - pair * a.pieces;
+        i += gridDim.x;
         const int src = a.copies[2 * pair], dst = a.copies[2 * pair + 1];
         if ((uint32_t)src >= (uint32_t)a.num_blocks || (uint32_t)dst >= (uint32_t)a.num_blocks) continue;
         const CopyLayer& l = a.layer[layer];
-        auto copy = [&](uint8_t* pool, uint32_t bytes) {
-            for (uint32_t at = 16 * threadIdx.x; at < bytes; at += 256 * 16)
-                *reinterpret_cast<copy_t*>(pool + (size_t)dst * bytes + at) = *reinterpret_cast<const copy_t*>(pool + (size_t)src * bytes + at);
+        auto copy_of = [&](uint8_t* k, uint8_t* v, uint32_t bytes, uint32_t at, auto f) {
+            if (at < 2 * bytes) {
+                uint8_t* pool = at < bytes ? k : v;
+                const uint32_t in = at < bytes ? at : at - bytes;
+                f(reinterpret_cast<const copy_t*>(pool + (size_t)src * bytes + in), reinterpret_cast<copy_t*>(pool + (size_t)dst * bytes + in));
+            }
         };
-        copy(l.k, a.kv_bytes);
-        copy(l.v, a.kv_bytes);
-        if (a.scale_bytes) {
-            copy((uint8_t*)l.ks, a.scale_bytes);
-            copy((uint8_t*)l.vs, a.scale_bytes);
-        }
+        copy_t x[4];
+#pragma unroll
+        for (uint32_t u = 0; u < 4; ++u)
+            copy_of(l.k, l.v, a.kv_bytes, piece * kCopyPiece + 16 * (256 * u + threadIdx.x),
+                    [&](const copy_t* from, copy_t*) { x[u] = __builtin_nontemporal_load(from); });
+        if (piece == 0 && a.scale_bytes)
+            for (uint32_t at = 16 * threadIdx.x; at < 2 * a.scale_bytes; at += 256 * 16)
+                copy_of((uint8_t*)l.ks, (uint8_t*)l.vs, a.scale_bytes, at, [&](const copy_t* from, copy_t* to) { *to = *from; });
+#pragma unroll
+        for (uint32_t u = 0; u < 4; ++u)
+            copy_of(l.k, l.v, a.kv_bytes, piece * kCopyPiece + 16 * (256 * u + threadIdx.x),
+                    [&](const copy_t*, copy_t* to) { __builtin_nontemporal_store(x[u], to); });
     }
 }
 
@@ -492,7 +539,8 @@ extern "C" int coopt_kv_blocks_free(const int32_t* seqs, int32_t num_listed, con
     if (num_listed == 0 || sh->num_seqs == 0) return COOPT_OK;
     if (!seqs || !tables || !lens || !refs || !free_map) return COOPT_ERR_NULL;
     const BlocksArgs a = blocks_args(tables, lens, refs, free_map, nullptr, sh);
-    hipLaunchKernelGGL(blocks_free_kernel, dim3((unsigned)num_listed), dim3(256), 0, (hipStream_t)hip_stream, a, seqs);
+    const int threads = sh->max_blocks_per_seq >= 1024 ? 1024 : (sh->max_blocks_per_seq + 63) / 64 * 64;
+    hipLaunchKernelGGL(blocks_free_kernel, dim3((unsigned)num_listed), dim3((unsigned)threads), 0, (hipStream_t)hip_stream, a, seqs);
     return launch_status();
 }
 
@@ -547,8 +595,10 @@ extern "C" int coopt_kv_blocks_fork(const int32_t* parents, const int32_t* child
     if (st != COOPT_OK) return st;
     hipStream_t stream = (hipStream_t)hip_stream;
     const BlocksArgs a = blocks_args(tables, lens, refs, free_map, workspace, sh);
-    hipLaunchKernelGGL(blocks_fork_kernel, dim3(1), dim3(kPlanThreads), 0, stream, a, parents, children, num_forks, copies, result);
-    if (num_forks > 0)
+    const bool few = (long long)num_forks * sh->max_blocks_per_seq <= kFewEntries;
+    hipLaunchKernelGGL(blocks_fork_kernel, dim3(1), dim3(kPlanThreads), 0, stream, a, parents, children, num_forks, copies, result,
+                       few ? 1 : 0);
+    if (!few)
         hipLaunchKernelGGL(blocks_share_kernel, dim3((unsigned)num_forks, row_workgroups(sh)), dim3(256), 0, stream, a, parents, children,
                            result);
     return launch_status();
@@ -566,8 +616,9 @@ extern "C" int coopt_kv_blocks_compact(int32_t* tables, const int32_t* lens, int
     if (st != COOPT_OK) return st;
     hipStream_t stream = (hipStream_t)hip_stream;
     const BlocksArgs a = blocks_args(tables, lens, refs, free_map, workspace, sh);
-    hipLaunchKernelGGL(blocks_compact_kernel, dim3(1), dim3(kPlanThreads), 0, stream, a, copies, num_copies);
-    if (sh->num_seqs > 0)
+    const bool few = (long long)sh->num_seqs * sh->max_blocks_per_seq <= kFewEntries;
+    hipLaunchKernelGGL(blocks_compact_kernel, dim3(1), dim3(kPlanThreads), 0, stream, a, copies, num_copies, few ? 1 : 0);
+    if (!few)
         hipLaunchKernelGGL(blocks_renumber_kernel, dim3((unsigned)sh->num_seqs, row_workgroups(sh)), dim3(256), 0, stream, a);
     return launch_status();
 }
@@ -585,7 +636,7 @@ extern "C" int coopt_kv_cache_copy_blocks(void* const* k_caches, void* const* v_
     for (int i = 0; i < num_layers; ++i)
         if (!k_caches[i] || !v_caches[i] || (scaled && (!k_scales[i] || !v_scales[i]))) return COOPT_ERR_NULL;
     const long long bytes = (long long)sh->num_kv_heads * kBlock * sh->head_dim * (scaled ? 1 : 2);
-    if (bytes > 0x7fffffffLL) return COOPT_ERR_SHAPE;
+    if (2 * bytes > 0x7fffffffLL) return COOPT_ERR_SHAPE;
     for (int l0 = 0; l0 < num_layers; l0 += kCopyLayers) {
         CopyArgs a{};
         a.copies = copies;
@@ -598,7 +649,9 @@ extern "C" int coopt_kv_cache_copy_blocks(void* const* k_caches, void* const* v_
         for (int i = 0; i < a.layers; ++i)
             a.layer[i] = CopyLayer{(uint8_t*)k_caches[l0 + i], (uint8_t*)v_caches[l0 + i], scaled ? k_scales[l0 + i] : nullptr,
                                    scaled ? v_scales[l0 + i] : nullptr};
-        const long long items = (long long)max_copies * a.layers;
+        a.pieces = (2 * a.kv_bytes + kCopyPiece - 1) / kCopyPiece;
+        const long long per_layer = (long long)max_copies * a.pieces, items = per_layer * a.layers;
+        if (per_layer > 0x7fffffffLL) return COOPT_ERR_SHAPE;
         hipLaunchKernelGGL(blocks_copy_kernel, dim3((unsigned)(items < 2048 ? items : 2048)), dim3(256), 0, (hipStream_t)hip_stream, a);
     }
     return launch_status();
