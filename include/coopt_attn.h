@@ -423,7 +423,8 @@ int coopt_paged_gqa_prefill_chunk_ws(const void* q, const void* k_cache, const v
  * A window of max_blocks_per_seq * 16 tokens or more hides nothing.  A launch reads what its rows see, to whole
  * blocks: the blocks behind every row's window, but for the first num_sinks tokens', are not read, nor
  * are their table entries (coopt_kv_blocks_free_outside_window gives them back to the pool and leaves -1 there).
- * Tokens that no row of a launch sees may hold anything; hidden scores never reach a result.
+ * Tokens that no row of a launch sees may hold anything; hidden scores never reach a result.  A sequence that
+ * gave blocks back is for these calls alone: the ones without a window read all of its blocks.
  *   window >= 1, num_sinks >= 0; COOPT_ERR_SHAPE otherwise
  *
  * Decode: one new token per sequence, at position context_lens[s] - 1.  Arguments as in

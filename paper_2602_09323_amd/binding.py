@@ -564,8 +564,13 @@ def _sized_workspace(workspace, need: int, what: str):
     return _dev(workspace, "workspace", what, need), _nbytes(workspace)
 
 
+def _window(window: int, num_sinks: int):
+    """Both as the library's 32-bit integers: a larger one is its largest, which hides, or leaves in sight, as much."""
+    return tuple(max(min(int(x), 2 ** 31 - 1), -1) for x in (window, num_sinks))
+
+
 def decode_window_workspace_bytes(shape: Shape, window: int, num_sinks: int) -> int:
-    return int(load_library().coopt_decode_window_workspace_bytes(ctypes.byref(shape), int(window), int(num_sinks)))
+    return int(load_library().coopt_decode_window_workspace_bytes(ctypes.byref(shape), *_window(window, num_sinks)))
 
 
 def paged_gqa_decode_window(q, k_cache, v_cache, k_scale, v_scale, block_tables, context_lens, window: int,
@@ -581,7 +586,7 @@ def paged_gqa_decode_window(q, k_cache, v_cache, k_scale, v_scale, block_tables,
     ins = _decode_inputs(q, k_cache, v_cache, k_scale, v_scale, block_tables, context_lens, z, what)
     pws, nws = _sized_workspace(workspace, decode_window_workspace_bytes(shape, window, num_sinks), what)
     _call("coopt_paged_gqa_decode_window",
-          *ins, int(window), int(num_sinks), _dev(out, "out", what, elem=2, min_bytes=z["q"]), pws, nws,
+          *ins, *_window(window, num_sinks), _dev(out, "out", what, elem=2, min_bytes=z["q"]), pws, nws,
           ctypes.byref(shape), _stream(stream))
 
 
@@ -601,13 +606,13 @@ def paged_gqa_decode_window_step(k, v, slot_mapping, q, k_cache, v_cache, k_scal
     ins = _decode_inputs(q, k_cache, v_cache, k_scale, v_scale, block_tables, context_lens, z, what)
     pws, nws = _sized_workspace(workspace, decode_window_workspace_bytes(shape, window, num_sinks), what)
     _call("coopt_paged_gqa_decode_window_step",
-          pk, pv, ps, *ins, int(window), int(num_sinks), _dev(out, "out", what, elem=2, min_bytes=z["q"]), pws, nws,
+          pk, pv, ps, *ins, *_window(window, num_sinks), _dev(out, "out", what, elem=2, min_bytes=z["q"]), pws, nws,
           ctypes.byref(shape), _stream(stream))
 
 
 def prefill_window_workspace_bytes(shape: Shape, max_chunk_len: int, window: int, num_sinks: int) -> int:
     return int(load_library().coopt_prefill_window_workspace_bytes(ctypes.byref(shape), int(max_chunk_len),
-                                                                   int(window), int(num_sinks)))
+                                                                   *_window(window, num_sinks)))
 
 
 def paged_gqa_prefill_chunk_window(q, k_cache, v_cache, k_scale, v_scale, block_tables, context_lens,
@@ -630,7 +635,7 @@ def paged_gqa_prefill_chunk_window(q, k_cache, v_cache, k_scale, v_scale, block_
     need = prefill_window_workspace_bytes(shape, max_chunk_len, window, num_sinks)
     pws, nws = _sized_workspace(workspace, need, what)
     _call("coopt_paged_gqa_prefill_chunk_window",
-          *ins, int(num_query_rows), int(max_chunk_len), int(window), int(num_sinks),
+          *ins, int(num_query_rows), int(max_chunk_len), *_window(window, num_sinks),
           _dev(out, "out", what, elem=2, min_bytes=rows_bytes), pws, nws, ctypes.byref(shape), _stream(stream))
 
 
@@ -772,7 +777,7 @@ def kv_blocks_free_outside_window(block_tables, context_lens, ref_counts, free_m
     if fast is not None and _entered(fast.free_window(block_tables, context_lens, ref_counts, free_map, window, num_sinks, shape, stream), "coopt_kv_blocks_free_outside_window"):
         return
     state = _block_state(block_tables, context_lens, ref_counts, free_map, shape, "kv_blocks_free_outside_window")
-    _call("coopt_kv_blocks_free_outside_window", *state, int(window), int(num_sinks), ctypes.byref(shape), _stream(stream))
+    _call("coopt_kv_blocks_free_outside_window", *state, *_window(window, num_sinks), ctypes.byref(shape), _stream(stream))
 
 
 def kv_blocks_compact(block_tables, context_lens, ref_counts, free_map, copies, num_copies, workspace, shape: Shape,
@@ -801,7 +806,8 @@ def kv_cache_copy_blocks(k_caches, v_caches, k_scales, v_scales, copies, num_cop
 
     def layers(pools):
         return [pools] if pools is None or hasattr(pools, "data_ptr") else list(pools)
-    n = len(layers(k_caches))
+    k_caches = layers(k_caches)
+    n = len(k_caches)
 
     def pointers(pools, name, need, optional=False):
         if optional and pools is None:
