@@ -58,8 +58,8 @@ namespace coopt {
 
 // window_tile.hip: one tile a workgroup.
 int launch_window_tiles(const void* q, const void* k_cache, const void* v_cache, const float* k_scale, const float* v_scale,
-                        const int32_t* block_tables, const int32_t* context_lens, const int32_t* query_start, int max_chunk_len,
-                        const Window& window, void* out, const coopt_shape* sh, int waves, hipStream_t stream);
+                        const int32_t* block_tables, const int32_t* context_lens, const int32_t* query_start, int num_query_rows,
+                        int max_chunk_len, const Window& window, void* out, const coopt_shape* sh, int waves, hipStream_t stream);
 
 struct PrefillArgs : PrefillDeal {
     const half_t* q;
@@ -962,7 +962,7 @@ extern "C" size_t coopt_prefill_window_workspace_bytes(const coopt_shape* sh, in
     if (check_shape(sh) != COOPT_OK || check_window(window, num_sinks) != COOPT_OK || max_chunk_len <= 0 || sh->num_seqs == 0)
         return 0;
     const Window w = window_of(sh, window, num_sinks);
-    if (window_tile_waves(sh, max_chunk_len, w) > 0) return 0;
+    if (window_tile_waves(sh, -1, max_chunk_len, w) > 0) return 0;
     return PrefillLaunchPlan(sh, max_chunk_len, true, window_row_tokens(sh, w)).workspace_bytes(sh);
 }
 
@@ -1039,10 +1039,10 @@ static int prefill_chunk(const void* q, const void* k_cache, const void* v_cache
         return COOPT_ERR_NULL;
     if (sh->kv_dtype != COOPT_KV_FP16 && (!k_scale || !v_scale)) return COOPT_ERR_NULL;
     if (window) {
-        const int waves = window_tile_waves(sh, max_chunk_len, *window);
+        const int waves = window_tile_waves(sh, num_query_rows, max_chunk_len, *window);
         if (waves > 0)
-            return launch_window_tiles(q, k_cache, v_cache, k_scale, v_scale, block_tables, context_lens, query_start, max_chunk_len,
-                                       *window, out, sh, waves, (hipStream_t)hip_stream);
+            return launch_window_tiles(q, k_cache, v_cache, k_scale, v_scale, block_tables, context_lens, query_start, num_query_rows,
+                                       max_chunk_len, *window, out, sh, waves, (hipStream_t)hip_stream);
     }
 
     PrefillArgs a{};

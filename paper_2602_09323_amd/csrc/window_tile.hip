@@ -1,12 +1,13 @@
-// Windowed prefill of few or short streams (window.hpp), in one launch without a workspace.
+// Windowed prefill of few rows or short streams (window.hpp), in one launch without a workspace.
 //
 // prefill.hip's workgroups carry 256 rows through LDS, which pays where streams are long; one that streams a stage
-// or two is mostly its own start and end, and a launch of few of them leaves CUs idle or needs parts and a merge.
-// Here a workgroup of WAVES wavefronts takes ONE tile, 16 rows of a head: the wavefronts take the groups of the tile's
-// view in turn, straight from the cache, with all but the first loads in flight under the arithmetic of
-// attn_tile.hpp, and meet in LDS.  What bounds it: the tile's round trips (rows and length, block numbers, tiles)
-// where there are few, and the L2 where there are many, since every tile reads its view for itself: a pair's
-// tiles sit on one XCD.
+// or two is mostly its own start and end, a launch of few of them leaves CUs idle or needs parts and a merge, and a
+// sequence of one row takes as long as one of fifty.  Here a workgroup of WAVES wavefronts takes ONE tile: 16 neighbouring
+// places of a pair's list of rows by head -- three rows of five heads, or all heads of a lone row, as in decode -- so
+// that its view is hardly longer than a window.  The wavefronts take the view's groups in turn, straight from the
+// cache, with all but the first loads in flight under the arithmetic of attn_tile.hpp, and meet in LDS.  What bounds
+// it: the tile's round trips (rows and length, block numbers, tiles) where there are few, and the L2 where there
+// are many, since every tile reads its view for itself.
 #include "attn_tile.hpp"
 #include "window_tile.hpp"
 
@@ -20,7 +21,7 @@ struct WindowTileArgs {
     const int32_t* query_start;
     half_t* out;
     int32_t H_q, H_k, G;
-    int32_t num_pairs, pair_tiles;      // tiles of a pair: rows, then heads
+    int32_t num_seqs, even_tiles;       // even_tiles > 0: every sequence has so many tiles a head
     int32_t max_blocks, pool_tiles;
     Window window;
     float scale_log2e;
@@ -33,31 +34,55 @@ window_tile_kernel(const WindowTileArgs a)
     constexpr int ES = BlockRegs<HEAD_DIM, KV>::ES;
     constexpr int DEPTH = HEAD_DIM * ES > 128 ? 2 : 3;      // groups in flight: 256 registers
     const int lane = threadIdx.x & 63, wave = wave_uniform((int)(threadIdx.x >> 6)), n = lane & 15, grp = lane >> 4;
-    // Ids go round-robin over 8 XCDs.  Where 8 divides the pairs, an XCD takes its share of them one after the other, all
-    // of a pair's tiles; otherwise tile by tile, which spreads the pairs evenly.  (One pair of 1008 tiles on
-    // one XCD: 22 us, so 7.)
-    const int id = (int)blockIdx.x;
-    int pair, tile;
-    if ((a.num_pairs & 7) == 0) {
-        const int k = (id >> 3) / a.pair_tiles;
-        tile = (id >> 3) - k * a.pair_tiles;
-        pair = 8 * k + (id & 7);
+    // Ids go round-robin over 8 XCDs.  Where 8 divides the heads, an XCD has its share of them, and a sequence's tiles of
+    // a head meet in its L2; where it divides the pairs of equal sequences, an XCD has its share of these; otherwise
+    // tiles are spread evenly.  (One pair of 1008 tiles on one XCD: 22 us, so 7.)
+    const int id = (int)blockIdx.x, r = id >> 3;
+    int g, slot, seq = 0, tile = -1;
+    if ((a.H_k & 7) == 0) {
+        const int share = a.H_k >> 3;
+        slot = r / share;
+        g = 8 * (r - slot * share) + (id & 7);
+    } else if (a.even_tiles > 0 && ((a.num_seqs * a.H_k) & 7) == 0) {
+        const int k = r / a.even_tiles, pair = 8 * k + (id & 7);
+        seq = pair / a.H_k;
+        g = pair - seq * a.H_k;
+        slot = seq * a.even_tiles + r - k * a.even_tiles;
     } else {
-        tile = id / a.num_pairs;
-        pair = id - tile * a.num_pairs;
+        slot = id / a.H_k;
+        g = id - slot * a.H_k;
     }
-    const int seq = pair / a.H_k, g = pair - seq * a.H_k;
-    const int i0 = 16 * (tile / a.G), head = g * a.G + tile % a.G;
+    // Slot -> sequence and tile.  A sequence that begins at row r has the slots from r G / 16 + its number on, which are
+    // as many as its tiles or one more: found by 64 lanes that look at 64 of them, of the whole, then of a 64th of it.
+    if (a.even_tiles > 0) {
+        seq = slot / a.even_tiles;
+        tile = slot - seq * a.even_tiles;
+    } else {
+        int left = a.num_seqs, first_slot = 0;
+        while (left > 1) {
+            const int step = (left + 63) >> 6, s = seq + lane * step;
+            const bool in = lane * step < left;
+            const int begin = in ? (int)(((long long)a.query_start[s] * a.G) >> 4) + s : 0;
+            const unsigned long long before = __builtin_amdgcn_ballot_w64(in && begin <= slot);
+            const int last = 63 - __builtin_clzll(before | 1ull);
+            seq += last * step;
+            first_slot = __builtin_amdgcn_readlane(begin, last);
+            left = min(step, left - last * step);
+        }
+        tile = slot - first_slot;
+    }
     const int qs = a.query_start[seq], C = a.query_start[seq + 1] - qs, t_ctx = a.context_lens[seq] - C;
-    if (i0 >= C) return;
-    const int row = min(i0 + n, C - 1);
+    const int places = C * a.G, p0 = 16 * tile;
+    if (tile < 0 || p0 >= places) return;
+    const int at_row = p0 / a.G, last_row = min(p0 + 15, places - 1) / a.G;
+    const int place = min(p0 + n, places - 1), row = place / a.G, head = g * a.G + place - row * a.G;
     half8_t q[HEAD_DIM / 32];
     load_q_operand<HEAD_DIM, KV>(q, a.q + ((size_t)(qs + row) * a.H_q + head) * HEAD_DIM, true, grp);
     // tokens up to the last row's, from the first row's window on
-    const WindowView v(a.window, t_ctx + min(i0 + 15, C - 1) + 1, t_ctx + i0 + 1 - a.window.size);
+    const WindowView v(a.window, t_ctx + last_row + 1, t_ctx + at_row + 1 - a.window.size);
     const int nb = (v.t + kBlock - 1) / kBlock, ng = (nb + 1) >> 1;
     const int limit = t_ctx + row + 1 - v.skip * kBlock;             // the lane's column sees tokens below this
-    const int seen_by_all = t_ctx + i0 + 1 - v.skip * kBlock;        // every column does
+    const int seen_by_all = t_ctx + at_row + 1 - v.skip * kBlock;    // every column does
     const int* bt = a.block_tables + (size_t)seq * a.max_blocks;
     auto group_of = [&](int e) { return e * WAVES + wave; };
     const int count = wave < ng ? min((ng - wave - 1) / WAVES + 1, kWindowTileGroups) : 0;
@@ -105,7 +130,7 @@ window_tile_kernel(const WindowTileArgs a)
     l += __shfl_xor(l, 16);
     l += __shfl_xor(l, 32);
     half_t* out = a.out + ((size_t)(qs + row) * a.H_q + head) * HEAD_DIM + 4 * grp;
-    const bool there = i0 + n < C;
+    const bool there = p0 + n < places;
     // (the caller's rows may begin at any 2-byte boundary)
     typedef _Float16 row_piece_t __attribute__((ext_vector_type(4), aligned(2)));
     auto store = [&](int c, floatx4 o, float inv) {
@@ -118,7 +143,7 @@ window_tile_kernel(const WindowTileArgs a)
 #pragma unroll
         for (int c = 0; c < HEAD_DIM / 16; ++c) store(c, acc[c], inv);
     } else {
-        // ---- the wavefronts' sums meet: lane (n, grp) has dims 16c + 4 grp .. of row n
+        // ---- the wavefronts' sums meet: lane (n, grp) has dims 16c + 4 grp .. of place n
         __shared__ __attribute__((aligned(16))) unsigned char sums[WAVES][HEAD_DIM / 16 * 1024 + 512];
         constexpr int kML = HEAD_DIM / 16 * 1024;
 #pragma unroll
@@ -142,7 +167,7 @@ window_tile_kernel(const WindowTileArgs a)
         const float inv = 1.0f / L;
 #pragma unroll
         for (int c0 = 0; c0 < HEAD_DIM / 16; c0 += WAVES) {
-            const int c = c0 + wave;                                // dims 16c .. +15 of every row
+            const int c = c0 + wave;                                // dims 16c .. +15 of every place
             if (c >= HEAD_DIM / 16) break;
             floatx4 o = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
@@ -176,8 +201,8 @@ static int launch_window_tiles(const WindowTileArgs& a, const coopt_shape* sh, u
 }
 
 int launch_window_tiles(const void* q, const void* k_cache, const void* v_cache, const float* k_scale, const float* v_scale,
-                        const int32_t* block_tables, const int32_t* context_lens, const int32_t* query_start, int max_chunk_len,
-                        const Window& window, void* out, const coopt_shape* sh, int waves, hipStream_t stream)
+                        const int32_t* block_tables, const int32_t* context_lens, const int32_t* query_start, int num_query_rows,
+                        int max_chunk_len, const Window& window, void* out, const coopt_shape* sh, int waves, hipStream_t stream)
 {
     WindowTileArgs a{};
     a.q = (const half_t*)q;
@@ -189,13 +214,16 @@ int launch_window_tiles(const void* q, const void* k_cache, const void* v_cache,
     a.H_q = sh->num_q_heads;
     a.H_k = sh->num_kv_heads;
     a.G = sh->num_q_heads / sh->num_kv_heads;
-    a.num_pairs = sh->num_seqs * sh->num_kv_heads;
+    a.num_seqs = sh->num_seqs;
     a.max_blocks = sh->max_blocks_per_seq;
     a.pool_tiles = sh->num_blocks * sh->num_kv_heads;
     a.window = window;
     a.scale_log2e = sh->softmax_scale * kLog2e;
-    a.pair_tiles = a.G * ((max_chunk_len + 15) / 16);
-    const unsigned wgs = (unsigned)a.num_pairs * (unsigned)a.pair_tiles;
+    const long long slots = window_tiles(sh, num_query_rows, max_chunk_len) / sh->num_kv_heads;
+    // (one sequence, or as many rows as all of them could have: no search)
+    if (sh->num_seqs == 1 || (long long)num_query_rows >= (long long)sh->num_seqs * max_chunk_len)
+        a.even_tiles = (int)(slots / sh->num_seqs);
+    const unsigned wgs = (unsigned)(slots * sh->num_kv_heads);
     if (waves == 1) return launch_window_tiles<1>(a, sh, wgs, stream);
     if (waves == 2) return launch_window_tiles<2>(a, sh, wgs, stream);
     return launch_window_tiles<4>(a, sh, wgs, stream);

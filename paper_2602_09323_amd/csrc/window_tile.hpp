@@ -26,31 +26,52 @@ inline double tile_us(const coopt_shape* sh, double tiles, int groups, int waves
     return 4.2 + std::max(own, chip) + 0.4 * std::min(own, chip);
 }
 
-// prefill.hip's launch: its plan's stages at 4 / 2.6 us (0.7 of it where a pair has 8 tiles at most), and the launch.
-inline double stream_us(const coopt_shape* sh, int max_chunk_len, long long tokens)
+// prefill.hip's launch: its plan's stages at 4 / 2.6 us (0.7 of it where a pair has 8 tiles at most), and the launch.  The
+// plan takes every chunk for the longest; where rows are missing, what is left of its workgroups counts, of which
+// every sequence has one per pair.
+inline double stream_us(const coopt_shape* sh, long long rows, int max_chunk_len, long long tokens)
 {
     const PrefillLaunchPlan plan(sh, max_chunk_len, true, tokens);
-    return 3.0 + (sh->head_dim == 128 ? 4.0 : 2.6) * (plan.nr == 1 ? 0.7 : 1.0) * plan.cost;
+    const int G = sh->num_q_heads / sh->num_kv_heads;
+    const double wgs = (double)sh->num_kv_heads * ((double)G * (double)rows / (16 * plan.wg_tiles) + sh->num_seqs);
+    const double stages = (double)(tokens + (plan.wg_tiles + G - 1) / G * 16) / kPrefillStageTokens;
+    const double real = (double)(long long)(wgs / kPrefillCUs + 1.0) * (2.3 + stages);
+    return 3.0 + (sh->head_dim == 128 ? 4.0 : 2.6) * (plan.nr == 1 ? 0.7 : 1.0) * std::min(plan.cost, real);
+}
+
+// Tiles of 16 places of a launch: of every sequence as many as the longest chunk has, or what that many rows have,
+// with a partly filled one per sequence.
+inline long long window_tiles(const coopt_shape* sh, long long rows, int max_chunk_len)
+{
+    const long long G = sh->num_q_heads / sh->num_kv_heads;
+    const long long even = sh->num_seqs * ((max_chunk_len * G + 15) / 16), found = rows * G / 16 + sh->num_seqs;
+    return sh->num_kv_heads * (sh->num_seqs == 1 || rows >= (long long)sh->num_seqs * max_chunk_len ? even : found);
 }
 
 // In us, 128 dims unless said, tiles (wavefronts a tile) / prefill.hip:
-//   40 heads over 8, E4M3     64 rows: window 64 5.8 (2) / 15.0, 256 7.1 (4) / 18.7, 1024 11.1 (4) / 23.1, 4096 23.8 (8) / 32.7
-//     256 rows                64 8.2 (1) / 15.3, 1024 22.3 (4) / 31.6, 4096 66.9 (8) / 46.6
+//   40 heads over 8, E4M3     64 rows: window 64 6.0 (2) / 15.0, 256 7.2 (4) / 18.7, 1024 11.4 (4) / 23.1, 4096 28.5 (4) / 32.7
+//     256 rows                64 7.8 (1) / 15.3, 1024 24.8 (2) / 31.6
 //     1000 rows               16 14.7 (1) / 14.7, 256 26.9 (1) / 23.0, 1024 61.6 (2) / 42.2
-//     4 x 512 rows            16 25.2 (1) / 26.5, 128 33.2 (1) / 36.0, 256 46.4 (1) / 43.9
-//   8 heads over 8, fp16      4 x 512 rows: 16 7.1 (1) / 18.5, 512 17.6 (1) / 32.6, 1024 31.3 (2) / 36.8, 4096 141 (8) / 58
-//   64 dims, 32 over 8, fp16  64 rows: 1024 8.0 (4) / 15.6   1000 rows: 16 7.7 (1) / 9.3, 512 17.4 (1) / 20.5, 1024 30.9 (4) / 31.5
-// Wavefronts per tile (1, 2 or 4; eight were no faster anywhere), or 0 where the launch is prefill.hip's.
-inline int window_tile_waves(const coopt_shape* sh, int max_chunk_len, const Window& window)
+//     4 x 512 rows            16 24.1 (1) / 26.5, 128 32.8 (1) / 36.0, 256 46.4 (1) / 43.9
+//     512 rows and 63 x 1     256 19.5 / 82.9, 1024 57.1 / 172.2, 4096 200 / 519
+//   8 heads over 8, fp16      4 x 512 rows: 16 7.0 (1) / 18.5, 512 22.4 (2) / 32.6, 1024 35.9 / 36.8
+//   64 dims, 32 over 8, fp16  64 rows: 1024 8.4 (4) / 15.6   1000 rows: 16 7.4 (1) / 9.3, 512 17.4 (1) / 20.5, 1024 30.9 (4) / 31.5
+// Wavefronts per tile (1, 2 or 4; eight were no faster anywhere), or 0 where the launch is prefill.hip's.  rows: of all
+// sequences, or less than 0 where only the longest chunk is known -- as to a caller who asks for a workspace: where
+// that already decides for tiles, there is none for anything else.
+inline int window_tile_waves(const coopt_shape* sh, long long rows, int max_chunk_len, const Window& window)
 {
-    const double tiles = (double)sh->num_seqs * sh->num_q_heads * ((max_chunk_len + 15) / 16);
+    const long long all = (long long)sh->num_seqs * max_chunk_len;
+    const bool known = rows >= 0 && rows < all;
     const int groups = (window_shape(sh, window, 16).max_blocks_per_seq + 1) / 2;
-    if (tiles > (double)kMaxWorkgroups) return 0;
-    double best_us = stream_us(sh, max_chunk_len, window_row_tokens(sh, window));
+    const long long tiles = window_tiles(sh, known ? rows : all, max_chunk_len);
+    if (tiles > kMaxWorkgroups) return 0;
+    double best_us = stream_us(sh, known ? rows : all, max_chunk_len, window_row_tokens(sh, window));
+    if (known && window_tile_waves(sh, -1, max_chunk_len, window) > 0) best_us = 1e30;
     int best = 0;
     for (int waves = 1; waves <= 4; waves *= 2) {
         if ((groups + waves - 1) / waves > kWindowTileGroups) continue;
-        const double us = tile_us(sh, tiles, groups, waves);
+        const double us = tile_us(sh, (double)tiles, groups, waves);
         if (us < best_us) {
             best_us = us;
             best = waves;

@@ -166,6 +166,24 @@ def test_prefill_in_every_form(oracle_mod, kv, H_q, H_k, d, chunks, lens, window
     assert_close(hip_prefill_window(w, cache_to_dev(cache), tables, q, starts, window, sinks), ref, f"{chunks[:3]} window {window}")
 
 
+@pytest.mark.parametrize("kv,H_q,H_k,d", HEADS + [("e4m3", 3, 3, 64), ("fp16", 24, 24, 64)])
+def test_mixed_batches(oracle_mod, kv, H_q, H_k, d):
+    """A chunk or two among many sequences of one row, of none, or of a few, as a server's step has them: in any order, and
+    more of them than a wavefront has lanes, more than lanes squared."""
+    rng = np.random.default_rng(23)
+    for S, longest, window, sinks in ((70, 200, 64, 4), (200, 130, 33, 0), (5000, 40, 16, 1)):
+        if S > 1000 and (H_q, d) != (16, 64):
+            continue
+        chunks = [int(x) for x in rng.choice([1, 1, 1, 1, 0, 2, 5], size=S)]
+        chunks[S // 3], chunks[S - 1], chunks[0] = longest, 1, 0
+        lens = [c + int(rng.integers(0, 150 if S < 1000 else 20)) for c in chunks]
+        w = random_workload("window_mixed", 24, kv, H_q, H_k, d, lens)
+        q, starts = ragged_rows(w, chunks)
+        cache, tables = poisoned(oracle_mod, w, hidden_from(w, chunks, window, sinks))
+        ref = window_attention(w, cache, q, w.context_lens, starts, window, sinks)
+        assert_close(hip_prefill_window(w, cache_to_dev(cache), tables, q, starts, window, sinks), ref, f"{S} sequences")
+
+
 @pytest.mark.parametrize("kv,H_q,H_k,d", HEADS[:2])
 def test_a_window_of_the_whole_context_is_plain_attention(oracle_mod, kv, H_q, H_k, d):
     w = random_workload("window_all", 15, kv, H_q, H_k, d, [700, 33, 1, 512])

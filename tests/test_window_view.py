@@ -100,7 +100,7 @@ int main()
                                     for (int width : {1, 70, 1 << 20}) {
                                         const coopt_shape sh = {seqs, hk * g, hk, d, 16, 1, width, kv, 1.0f};
                                         const Window w = window_of(&sh, window, sinks);
-                                        const int waves = window_tile_waves(&sh, chunk, w);
+                                        const int waves = window_tile_waves(&sh, -1, chunk, w);
                                         const int groups = (window_shape(&sh, w, 16).max_blocks_per_seq + 1) / 2;
                                         if (waves < 0 || waves > 4 || (waves & (waves - 1))) printf("%d wavefronts\n", waves);
                                         if (waves && (groups + waves - 1) / waves > kWindowTileGroups) printf("%d groups for %d\n", groups, waves);
@@ -109,15 +109,15 @@ int main()
 }
 """
 
-# what the cases of test_gpu_window.py reach: (kv, q heads, kv heads, dim, sequences, longest chunk, table, window, sinks)
+# what the cases of test_gpu_window.py reach: (kv, q heads, kv heads, dim, sequences, longest chunk, table, window, sinks, rows)
 FORMS = r"""
 int main()
 {
-    int a[9];
-    while (scanf("%d %d %d %d %d %d %d %d %d", a, a + 1, a + 2, a + 3, a + 4, a + 5, a + 6, a + 7, a + 8) == 9) {
+    int a[10];
+    while (scanf("%d %d %d %d %d %d %d %d %d %d", a, a + 1, a + 2, a + 3, a + 4, a + 5, a + 6, a + 7, a + 8, a + 9) == 10) {
         const coopt_shape sh = {a[4], a[1], a[2], a[3], 16, 1, a[6], a[0], 1.0f};
         const Window w = window_of(&sh, a[7], a[8]);
-        const int waves = window_tile_waves(&sh, a[5], w);
+        const int waves = window_tile_waves(&sh, a[9], a[5], w);
         const PrefillLaunchPlan plan(&sh, a[5], true, window_row_tokens(&sh, w));
         if (waves) printf("tile%d\n", waves);
         else printf("stream%d%s\n", plan.wg_tiles, plan.parts > 1 ? "parts" : "");
@@ -146,7 +146,7 @@ def test_every_form_has_its_cases(tmp_path):
     lines = []
     for kv, H_q, H_k, d in cases.FORM_HEADS:
         for chunks, lens, window, sinks in cases.FORM_CASES:
-            lines.append((kinds[kv], H_q, H_k, d, len(lens), max(chunks), -(-max(lens) // 16), window, sinks))
+            lines.append((kinds[kv], H_q, H_k, d, len(lens), max(chunks), -(-max(lens) // 16), window, sinks, sum(chunks)))
     said = subprocess.run([program], input="\n".join(" ".join(map(str, x)) for x in lines), check=True, capture_output=True,
                           text=True).stdout.split()
     for kv in range(3):
