@@ -1,6 +1,8 @@
 """GPU: the operators on the pool's blocks against a model of lists and loops, every table entry, length, reference
 count, map word, slot and pair exactly, and what they must leave alone left alone: entries that no sequence holds are
 filled with numbers that name no block."""
+import ctypes
+
 import numpy as np
 import pytest
 import torch
@@ -178,6 +180,29 @@ def test_fork():
     dev.outside(pool, 20, 16)
     dev.fork(pool, [4], [0], "of a sequence with blocks behind its window")
     assert int(dev.result) == 0
+
+
+def test_no_sequences_and_no_forks():
+    """What is then not needed may be NULL, and nothing is read through it."""
+    lib, none = coopt.load_library(), ctypes.c_void_p(None)
+    shape = coopt.Shape(3, 2, 2, 64, 16, 4000, 10, coopt.COOPT_KV_E4M3, 0.125)
+    ws = torch.empty(coopt.kv_blocks_workspace_bytes(shape), dtype=torch.uint8, device="cuda")
+    result = torch.tensor([7, 7], dtype=torch.int32, device="cuda")
+    starts = torch.tensor([0, 5], dtype=torch.int32, device="cuda")
+    stream = ctypes.c_void_p(torch.cuda.current_stream().cuda_stream)
+    ptr = [ctypes.c_void_p(t.data_ptr()) for t in (ws, result, result[1:], starts[1:])]
+
+    def reserve(starts_at, rows):
+        shape.num_seqs = 0
+        assert lib.coopt_kv_blocks_reserve(starts_at, rows, none, none, none, none, none, ptr[1], ptr[0],
+                                           ctypes.c_size_t(ws.numel()), ctypes.byref(shape), stream) == 0
+        return int(result[0])
+    assert reserve(none, 0) == 0 and reserve(none, 9) == 0 and reserve(none, 9000) == 0
+    assert reserve(ptr[3], 9) == -1 and reserve(ptr[3], 9000) == -1                          # (does not begin at 0)
+    shape.num_seqs = 3
+    assert lib.coopt_kv_blocks_fork(none, none, 0, none, none, none, none, none, ptr[2], ptr[0],
+                                    ctypes.c_size_t(ws.numel()), ctypes.byref(shape), stream) == 0
+    assert int(result[1]) == 0
 
 
 def test_fork_without_room():
