@@ -59,7 +59,7 @@ namespace coopt {
 // window_tile.hip: one tile a workgroup.
 int launch_window_tiles(const void* q, const void* k_cache, const void* v_cache, const float* k_scale, const float* v_scale,
                         const int32_t* block_tables, const int32_t* context_lens, const int32_t* query_start, int num_query_rows,
-                        int max_chunk_len, const Window& window, void* out, const coopt_shape* sh, int waves, hipStream_t stream);
+                        int max_chunk_len, const Window& window, void* out, const coopt_shape* sh, int waves, int sets, hipStream_t stream);
 
 struct PrefillArgs : PrefillDeal {
     const half_t* q;
@@ -1042,10 +1042,11 @@ static int prefill_chunk(const void* q, const void* k_cache, const void* v_cache
         return COOPT_ERR_NULL;
     if (sh->kv_dtype != COOPT_KV_FP16 && (!k_scale || !v_scale)) return COOPT_ERR_NULL;
     if (window) {
-        const int waves = window_tile_waves(sh, num_query_rows, max_chunk_len, *window);
+        int sets = 1;
+        const int waves = window_tile_waves(sh, num_query_rows, max_chunk_len, *window, &sets);
         if (waves > 0)
             return launch_window_tiles(q, k_cache, v_cache, k_scale, v_scale, block_tables, context_lens, query_start, num_query_rows,
-                                       max_chunk_len, *window, out, sh, waves, (hipStream_t)hip_stream);
+                                       max_chunk_len, *window, out, sh, waves, sets, (hipStream_t)hip_stream);
     }
 
     PrefillArgs a{};

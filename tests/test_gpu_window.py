@@ -153,7 +153,7 @@ def test_prefill_of_longer_chunks(oracle_mod, kv, H_q, H_k, d, chunks, lens, win
 FORM_HEADS = [("e4m3", 40, 8, 128), ("e4m3", 32, 8, 64), ("e5m2", 40, 8, 128), ("e5m2", 32, 8, 64), ("fp16", 16, 8, 128), ("fp16", 32, 8, 64)]
 FORM_CASES = [([30, 7], [800, 90], 130, 4), ([16], [700], 500, 4), ([16], [2500], 2400, 4), ([16, 16], [4300, 60], 4000, 7),
               ([40] * 10 + [5], [40] * 10 + [5], 16, 0), ([1500, 40], [3500, 2500], 900, 20), ([700], [5000], 4100, 4),
-              ([500] * 5, [500] * 5, 33, 4)]
+              ([500] * 5, [500] * 5, 33, 4), ([200], [300], 16, 0)]
 
 
 @pytest.mark.parametrize("chunks,lens,window,sinks", FORM_CASES)

@@ -100,8 +100,10 @@ int main()
                                     for (int width : {1, 70, 1 << 20}) {
                                         const coopt_shape sh = {seqs, hk * g, hk, d, 16, 1, width, kv, 1.0f};
                                         const Window w = window_of(&sh, window, sinks);
-                                        const int waves = window_tile_waves(&sh, -1, chunk, w);
-                                        const int groups = (window_shape(&sh, w, 16).max_blocks_per_seq + 1) / 2;
+                                        int sets = 1;
+                                        const int waves = window_tile_waves(&sh, -1, chunk, w, &sets);
+                                        if (sets < 1 || sets > 2 || (sets == 2 && (waves != 1 || (kv == 0 && d == 128)))) printf("%d sets\n", sets);
+                                        const int groups = (window_shape(&sh, w, 16 * sets).max_blocks_per_seq + 1) / 2;
                                         if (waves < 0 || waves > 4 || (waves & (waves - 1))) printf("%d wavefronts\n", waves);
                                         if (waves && (groups + waves - 1) / waves > kWindowTileGroups) printf("%d groups for %d\n", groups, waves);
                                     }
@@ -117,9 +119,10 @@ int main()
     while (scanf("%d %d %d %d %d %d %d %d %d %d", a, a + 1, a + 2, a + 3, a + 4, a + 5, a + 6, a + 7, a + 8, a + 9) == 10) {
         const coopt_shape sh = {a[4], a[1], a[2], a[3], 16, 1, a[6], a[0], 1.0f};
         const Window w = window_of(&sh, a[7], a[8]);
-        const int waves = window_tile_waves(&sh, a[9], a[5], w);
+        int sets = 1;
+        const int waves = window_tile_waves(&sh, a[9], a[5], w, &sets);
         const PrefillLaunchPlan plan(&sh, a[5], true, window_row_tokens(&sh, w));
-        if (waves) printf("tile%d\n", waves);
+        if (waves) printf("tile%d%s\n", waves, sets == 2 ? "of32" : "");
         else printf("stream%d%s\n", plan.wg_tiles, plan.parts > 1 ? "parts" : "");
     }
     return 0;
@@ -153,6 +156,7 @@ def test_every_form_has_its_cases(tmp_path):
         for d in (64, 128):
             found = {s for s, x in zip(said, lines) if x[0] == kv and x[3] == d}
             assert {"tile1", "tile2", "tile4"} <= found, (kv, d, found)
+            assert "tile1of32" in found or (kv == 0 and d == 128), (kv, d, found)
             assert {x[:8] for x in found} >= {"stream16"} and {x[:7] for x in found} >= {"stream8"}, (kv, d, found)
     assert {"stream16", "stream16parts", "stream8parts"} <= set(said)
 
