@@ -486,8 +486,10 @@ int coopt_paged_gqa_prefill_chunk_window(const void* q, const void* k_cache, con
  * a list is left out, as a negative slot is.  num_q_heads, head_dim, kv_dtype and softmax_scale of the shape do not
  * matter, but have to be valid.
  *   result (device, int32 [1])   0: done; n > 0: n blocks too few were free; -1: an argument in device memory
- *                                out of its range.  Where it is not 0 nothing has been changed, and slots and
- *                                copies are all -1, so that the calls which take them do nothing.
+ *                                out of its range.  Where it is not 0 nothing has been changed, and no slot of the
+ *                                num_query_rows names a place (-1; behind the last sequence's rows a slot that was
+ *                                negative stays as it was) and copies are all -1, so that the calls which take them
+ *                                do nothing.
  *   workspace  coopt_kv_blocks_workspace_bytes(shape) bytes, 16-byte aligned, contents undefined before and after
  *
  * init: ref_counts and free_map from tables and lengths (lengths of 0: an empty pool).
@@ -501,8 +503,9 @@ int coopt_kv_blocks_init(const int32_t* block_tables, const int32_t* context_len
  * query_start [num_seqs+1] from 0, increasing, its last at most num_query_rows) -- or, with query_start NULL, one where
  * context_lens[s] > 0 and none elsewhere, row s being sequence s's (num_query_rows >= num_seqs).  New table entries
  * name free blocks (of sequences, then of entries, in order), context_lens counts the new tokens, and
- * slot_mapping [num_query_rows] int64 gets every row's slot (-1 for a sequence without tokens; rows from
- * query_start[num_seqs] on are left as they were): the arguments of the cache write and the attention that follow.
+ * slot_mapping [num_query_rows] int64 gets every row's slot (-1 for a sequence without tokens; rows behind the last
+ * sequence's -- from query_start[num_seqs] on, or num_seqs -- are left as they were, so a write over all of them wants these
+ * negative): the arguments of the cache write and the attention that follow.
  * result -1: a sequence would outgrow its row of the table, or query_start is none.  A sequence that grows inside its
  * last block must hold it alone (as after fork).
  */

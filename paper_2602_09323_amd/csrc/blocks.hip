@@ -198,6 +198,13 @@ __device__ __forceinline__ int64_t slot_of(const BlocksArgs& a, int s, int pos)
     return (int64_t)a.tables[(size_t)s * a.max_blocks + pos / kBlock] * kBlock + pos % kBlock;
 }
 
+// Where nothing is reserved, no row keeps a slot that a write would take: -1, also over what an earlier step left in
+// the rows behind the last sequence's (which a reservation leaves alone; negative ones stay).
+__device__ __forceinline__ void refuse_slot(int64_t* slots, int r, int rows)
+{
+    if (r < rows || slots[r] >= 0) slots[r] = -1;
+}
+
 // SLOTS: the rows' slots, too (few rows; else blocks_slots_kernel behind this).
 template <bool SLOTS>
 __global__ void __launch_bounds__(kPlanThreads)
@@ -228,9 +235,8 @@ blocks_reserve_kernel(const BlocksArgs a, const int32_t* starts, int num_rows, i
     if (threadIdx.x == 0) *result = missing;
     const int rows = starts ? min(max(starts[a.num_seqs], 0), num_rows) : a.num_seqs;
     if (missing != 0) {
-        // nothing is reserved: slots that the writes leave out
         if (SLOTS)
-            for (int r = threadIdx.x; r < rows; r += kPlanThreads) slots[r] = -1;
+            for (int r = threadIdx.x; r < num_rows; r += kPlanThreads) refuse_slot(slots, r, rows);
         return;
     }
     // the new blocks' places in the tables
@@ -256,11 +262,12 @@ blocks_slots_kernel(const BlocksArgs a, const int32_t* starts, int num_rows, int
 {
     const int r = blockIdx.x * 256 + threadIdx.x;
     const int rows = starts ? min(starts[a.num_seqs], num_rows) : a.num_seqs;
-    if (r >= rows) return;
+    if (r >= num_rows) return;
     if (*result != 0) {
-        slots[r] = -1;
+        refuse_slot(slots, r, rows);
         return;
     }
+    if (r >= rows) return;
     const int s = starts ? last_not_above(a.num_seqs, r, [&](int i) { return starts[i]; }) : r;
     const int t = a.lens[s];
     slots[r] = t > 0 ? slot_of(a, s, starts ? t - (starts[s + 1] - r) : t - 1) : -1;
@@ -573,7 +580,10 @@ extern "C" int coopt_kv_blocks_reserve(const int32_t* query_start, int32_t num_q
     if (st != COOPT_OK) return st;
     hipStream_t stream = (hipStream_t)hip_stream;
     BlocksArgs a = blocks_args(tables, lens, refs, free_map, workspace, sh);
-    if (sh->num_seqs == 0) a.words = num_query_rows = 0;        // (the map may be NULL, and so may the slots)
+    if (sh->num_seqs == 0) {                                    // (the map may be NULL, and so may the slots)
+        a.words = 0;
+        if (!slot_mapping) num_query_rows = 0;
+    }
     if (num_query_rows <= 4 * kPlanThreads) {
         hipLaunchKernelGGL(blocks_reserve_kernel<true>, dim3(1), dim3(kPlanThreads), 0, stream, a, query_start, num_query_rows,
                            slot_mapping, result);
