@@ -55,6 +55,9 @@ struct CacheView {
 // inside fp16's normal range for value rows of ordinary magnitude, and at most 2^15 * 65504/57344.
 constexpr float kPShift = 6.0f;                     // (chunked prefill: v_scale is in the exponent there)
 constexpr float kRescaleSlack = 2.0f;
+// The reference of a stream before its first score.  Finite, not -inf: all that a column sees of its first groups may be
+// scores of -inf (infinite keys), or nothing at all, and exp2(-inf - m) is then to be 0, not exp2(-inf + inf).
+constexpr float kNoScore = -0x1.fffffep127f;
 template <int KV> constexpr float kPShiftOf = KV == COOPT_KV_E5M2 ? 13.0f : 6.0f;
 template <int KV> constexpr float kPUnshiftOf = KV == COOPT_KV_E5M2 ? 1.0f / 8192.0f : 1.0f / 64.0f;
 
@@ -435,7 +438,7 @@ __device__ __forceinline__ void group_pv(const BlockRegs<HEAD_DIM, KV>& A,
 //   m: reference max of column n in log2 units (within kRescaleSlack of the true running max),
 //      identical in the four lanes (n, 0..3).
 //   l: this lane's share of the running sum, acc[c][r] = O^T[16c + 4grp + r][n], both times 2^kPShiftOf<KV>.
-// Requirement: whenever m is still -inf, the group holds a token visible to column n.
+// m begins at kNoScore (a stream that begins at -inf needs a score above it in its first group).
 template <int HEAD_DIM, int KV, bool HOLES = false>
 __device__ __forceinline__ void group_update(BlockRegs<HEAD_DIM, KV>& A, BlockRegs<HEAD_DIM, KV>& B,
                                              const half8_t (&qop)[HEAD_DIM / 32], float& m, float& l,
@@ -451,7 +454,7 @@ __device__ __forceinline__ void group_update(BlockRegs<HEAD_DIM, KV>& A, BlockRe
         float nm = fmaxf(bm, __shfl_xor(bm, 16));
         nm = fmaxf(nm, __shfl_xor(nm, 32));
         nm = fmaxf(nm, m);
-        const float alpha = __builtin_amdgcn_exp2f(m - nm);   // m = -inf at the start gives 0
+        const float alpha = __builtin_amdgcn_exp2f(m - nm);   // m = kNoScore at the start gives 0
         l *= alpha;
 #pragma unroll
         for (int c = 0; c < HEAD_DIM / 16; ++c) acc[c] *= alpha;
@@ -488,7 +491,7 @@ __device__ __forceinline__ void group_update_block_reduce(
                       fmaxf(fmaxf(z[4], z[5]), fmaxf(z[6], z[7])));
     __syncthreads();
     const float nm = fmaxf(m, fmaxf(fmaxf(red[n], red[16 + n]), fmaxf(red[32 + n], red[48 + n])));
-    const float alpha = __builtin_amdgcn_exp2f(m - nm);       // m = -inf at the start gives 0
+    const float alpha = __builtin_amdgcn_exp2f(m - nm);       // m = kNoScore at the start gives 0
     m = nm;
     const float mm = m - kPShiftOf<KV>;
     float p[8], ps = 0.0f;

@@ -659,7 +659,7 @@ __device__ __forceinline__ void stream_share(const FlatArgs& a, Source& src, uns
     PartialSlot parked;
     parked.row0 = -1;
     half8_t q_cur[HEAD_DIM / 32];
-    float m = -INFINITY, l = 0.0f;
+    float m = kNoScore, l = 0.0f;
     floatx4 acc[HEAD_DIM / 16];
 #pragma unroll
     for (int c = 0; c < HEAD_DIM / 16; ++c) acc[c] = floatx4{0.f, 0.f, 0.f, 0.f};
@@ -742,7 +742,7 @@ __device__ __forceinline__ void stream_share(const FlatArgs& a, Source& src, uns
                         const PartialSlot ps = src.slot(e);
                         l += __shfl_xor(l, 16);
                         l += __shfl_xor(l, 32);
-                        const float inv = 1.0f / l;
+                        const float inv = l != 0.0f ? 1.0f / l : 0.0f;   // (zeros of weight zero)
                         if (c0 + e == total - 1) {
                             // end of the share: nothing runs behind these stores
 #pragma unroll
@@ -760,7 +760,7 @@ __device__ __forceinline__ void stream_share(const FlatArgs& a, Source& src, uns
                             *reinterpret_cast<float*>(park + kParkAcc + 4 * lane) = m * kLn2;
                             *reinterpret_cast<float*>(park + kParkAcc + 256 + 4 * lane) = l * kPUnshiftOf<KV>;
                             parked = ps;
-                            m = -INFINITY;
+                            m = kNoScore;
                             l = 0.0f;
 #pragma unroll
                             for (int c = 0; c < HEAD_DIM / 16; ++c) acc[c] = floatx4{0.f, 0.f, 0.f, 0.f};
@@ -1201,8 +1201,7 @@ pair_decode_kernel(const FlatArgs a)
         loader.issue(r[1], (b + 1 < nb ? __builtin_amdgcn_readlane(ids, 2 * ee + 1) : 0) * a.H_k + g, e < count && b + 1 < nb);
     };
     __shared__ __attribute__((aligned(16))) unsigned char sums[kWaves][HEAD_DIM / 16 * 1024 + 512];
-    // (finite, not -inf: all scores of a wavefront's first group may be -inf, which is then often its only one)
-    float m = -0x1.fffffep127f, l = 0.0f;
+    float m = kNoScore, l = 0.0f;
     floatx4 acc[HEAD_DIM / 16];
 #pragma unroll
     for (int c = 0; c < HEAD_DIM / 16; ++c) acc[c] = floatx4{0.f, 0.f, 0.f, 0.f};

@@ -211,12 +211,11 @@ window_tile_kernel(const WindowTileArgs a)
         loader.issue(r[0], e < count ? idA * a.H_k + g : g, e < count);
         loader.issue(r[1], e < count && b + 1 < nb ? idB * a.H_k + g : g, e < count && b + 1 < nb);
     };
-    // (finite: a column may see nothing of a wavefront's groups)
     float m[SETS], l[SETS];
     floatx4 acc[SETS][HEAD_DIM / 16];
 #pragma unroll
     for (int u = 0; u < SETS; ++u) {
-        m[u] = -0x1.fffffep127f;
+        m[u] = kNoScore;
         l[u] = 0.0f;
 #pragma unroll
         for (int c = 0; c < HEAD_DIM / 16; ++c) acc[u][c] = floatx4{0.f, 0.f, 0.f, 0.f};
