@@ -438,7 +438,7 @@ __device__ __forceinline__ void group_pv(const BlockRegs<HEAD_DIM, KV>& A,
 //   m: reference max of column n in log2 units (within kRescaleSlack of the true running max),
 //      identical in the four lanes (n, 0..3).
 //   l: this lane's share of the running sum, acc[c][r] = O^T[16c + 4grp + r][n], both times 2^kPShiftOf<KV>.
-// m begins at kNoScore (a stream that begins at -inf needs a score above it in its first group).
+// m begins at kNoScore.
 template <int HEAD_DIM, int KV, bool HOLES = false>
 __device__ __forceinline__ void group_update(BlockRegs<HEAD_DIM, KV>& A, BlockRegs<HEAD_DIM, KV>& B,
                                              const half8_t (&qop)[HEAD_DIM / 32], float& m, float& l,

@@ -87,7 +87,7 @@ paged_decode_kernel(const DecodeArgs a)
     load_q_operand<HEAD_DIM, KV>(qop, a.q + ((size_t)seq * a.H_q + g * a.G + n) * HEAD_DIM,
                                  n < a.G, grp);
 
-    float m = -INFINITY, l = 0.0f;
+    float m = kNoScore, l = 0.0f;
     floatx4 acc[HEAD_DIM / 16];
 #pragma unroll
     for (int c = 0; c < HEAD_DIM / 16; ++c) acc[c] = floatx4{0.f, 0.f, 0.f, 0.f};
@@ -164,11 +164,12 @@ paged_decode_kernel(const DecodeArgs a)
         for (int w = 0; w < nwaves; ++w) M = fmaxf(M, sm_m[w * 16 + hh]);
         float L = 0.0f, O = 0.0f;
         for (int w = 0; w < nwaves; ++w) {
-            const float f = __builtin_amdgcn_exp2f(sm_m[w * 16 + hh] - M);  // idle waves: 0
-            L += sm_l[w * 16 + hh] * f;
+            const float f = __builtin_amdgcn_exp2f(sm_m[w * 16 + hh] - M);
+            L += sm_l[w * 16 + hh] * f;                  // idle waves, and those that saw only -inf: 0
             O += sm_acc[(w * a.G + hh) * HEAD_DIM + dim] * f;
         }
-        const float o = O / L;                           // the common power of two of O and L cancels
+        // (the common power of two of O and L cancels; a partition without weights leaves zeros of weight zero)
+        const float o = a.direct || L != 0.0f ? O / L : 0.0f;
         const size_t row = (size_t)seq * a.H_q + g * a.G + hh;
         if (a.direct) {
             a.out[row * HEAD_DIM + dim] = (half_t)o;

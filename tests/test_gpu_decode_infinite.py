@@ -7,8 +7,9 @@ import torch
 
 import paper_2602_09323_amd as coopt
 import workloads
-from gpu_utils import assert_close, cache_to_dev, dev, hip_decode, planned, shape_of
+from gpu_utils import assert_close, cache_to_dev, hip_decode, planned, shape_of
 from helpers import oracle_fill
+from test_gpu_partitioned import _hip_partitioned
 from test_gpu_scheduled import _prepare, _run
 from test_gpu_window import hip_decode_window
 from window_utils import random_workload, window_attention
@@ -99,3 +100,22 @@ def test_balanced(oracle_mod, H_q, H_k, d, plan):
     dcache = cache_to_dev(cache)
     _check(hip_decode(w, dcache), ref, f"plan {plan}")
     _check(_run(w, dcache, _prepare(w)), ref, f"prepared, plan {plan}")
+
+
+def test_without_a_workspace(oracle_mod):
+    w, cache, ref = _whole(oracle_mod, 70)
+    _check(hip_decode(w, cache_to_dev(cache), split=False), ref, "no workspace")
+
+
+@pytest.mark.parametrize("P", [32, 64, 512])
+@pytest.mark.parametrize("waves", [1, 4])
+def test_partitions(oracle_mod, P, waves):
+    """Partitions that begin with such a group, of nothing else, and wavefronts of a partition that see nothing else."""
+    w, cache, ref = _whole(oracle_mod, 6)
+    planned.set_plan(waves_per_group=waves)
+    out, tmp, ml, es = _hip_partitioned(w, cache_to_dev(cache), P, -(-int(w.context_lens.max()) // P))
+    _check(out, ref, f"partitions of {P}")
+    if P == 64:                                                # of tokens 64 .. 127, heads that give them no weight
+        G = w.H_q // w.H_k
+        none = slice(2 * G, 3 * G, 2)
+        assert (es[:, none, 1] == 0).all() and (tmp[:, none, 1] == 0).all() and np.isfinite(ml[:, none, 1]).all()
