@@ -175,13 +175,12 @@ blocks_free_window_kernel(const BlocksArgs a, int window, int sinks)
     const int lead = (sinks + kBlock - 1) / kBlock;
     for (int top = min((a.lens[s] - window) / kBlock, a.max_blocks); top > lead; top -= 64) {
         const int b = top - 1 - lane;
-        const bool there = b >= lead;
-        const int id = there ? row[b] : 0;
-        if (there && id >= 0) {
+        const int id = b >= lead ? row[b] : 0;
+        if (b >= lead && is_block(a, id)) {        // (another entry is not the sequence's)
             release(a, id);
             row[b] = -1;
         }
-        if (__builtin_amdgcn_ballot_w64(there && id < 0)) break;
+        if (__builtin_amdgcn_ballot_w64(id == -1)) break;
     }
 }
 
