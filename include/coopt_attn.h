@@ -424,7 +424,8 @@ int coopt_paged_gqa_prefill_chunk_ws(const void* q, const void* k_cache, const v
  * blocks: the blocks behind every row's window, but for the first num_sinks tokens', are not read, nor
  * are their table entries (coopt_kv_blocks_free_outside_window gives them back to the pool and leaves -1 there).
  * Tokens that no row of a launch sees may hold anything; hidden scores never reach a result.  A sequence that
- * gave blocks back is for these calls alone: the ones without a window read all of its blocks.
+ * gave blocks back is for these calls alone, with no larger window and no more sinks than it gave them back for: the
+ * entries of what a row sees must name blocks (not checked), and the calls without a window read all of a sequence's.
  *   window >= 1, num_sinks >= 0; COOPT_ERR_SHAPE otherwise
  *
  * Decode: one new token per sequence, at position context_lens[s] - 1.  Arguments as in
@@ -455,7 +456,10 @@ int coopt_paged_gqa_decode_window_step(const void* k, const void* v, const int64
 
 /*
  * Chunked prefill through the window: local row i of sequence s is at position context_lens[s] - C_s + i.
- * Arguments as in coopt_paged_gqa_prefill_chunk_ws.
+ * Arguments as in coopt_paged_gqa_prefill_chunk_ws.  One of two launches runs, as the shape, max_chunk_len, num_query_rows
+ * and the window say: one rounds every weight to fp16, as coopt_paged_gqa_prefill_chunk does (rows 2.5e-4 to 2.9e-4 of
+ * their norm off the definition in 64 bits), the other keeps it as two fp16 parts, as decode does (2.1e-4, which is
+ * what rounding the output leaves).  So a row's last bits depend on the call that it is in.
  *   workspace  coopt_prefill_window_workspace_bytes(shape, max_chunk_len, window, num_sinks) bytes, 16-byte
  *              aligned; NULL where that is 0
  */

@@ -444,7 +444,7 @@ constexpr uint32_t kCopyPiece = 16384;         // bytes a workgroup has in fligh
 
 // A piece of a block's K and V in one layer at a time, the scales with the first; all of a piece's loads are asked for
 // before its first store.  Bound by HBM where there are enough pieces to fill the chip: 4.85 GB (both ways) of a
-// compaction in 16 layers 928 us, 5.2 TB/s; one block of 8 samples in 40 layers, 21.6 MB, 6.1 us.  (A workgroup per block
+// compaction in 16 layers 906 to 928 us, 5.2 to 5.4 TB/s; one block of 8 samples in 40 layers, 21.6 MB, 6.1 us.  (A workgroup per block
 // and layer that copied K, then V, 4 KB at a time: 1017 us and 7.1.)
 __global__ void __launch_bounds__(256)
 blocks_copy_kernel(const CopyArgs a)

@@ -797,7 +797,9 @@ __device__ __forceinline__ int share_of_workgroup(int wg, int n)
 // One wave per workgroup.  The block numbers of up to 32 groups come from one gathered vector load
 // (lane 2j+h = block h of the j-th group), whatever pairs they belong to.
 // Through a window (WINDOW; 64 sequences of up to 32 000 tokens through 4096 + 4, 40 heads over 8, E4M3: 530 MB) the launch
-// takes 85 us, 6.2 TB/s: bound by HBM as without.
+// takes 85 us, 6.2 TB/s: bound by HBM as without; with the new tokens (APPEND) 87 us, E5M2 89, and the merge that stores them
+// 5.4.  A pass of the fused step 90.6 us, of decode alone 87.6, of write and decode apart 91.0; 32 sequences through
+// 1024 + 4 over an fp16 cache (131 MB) 31.1, 29.6 and 32.2.
 template <int HEAD_DIM, int KV, int DEPTH, bool BIG, bool BLOCK_REDUCE, bool APPEND, bool WINDOW = false>
 __global__ void __launch_bounds__(64)
 flat_stream_kernel(const FlatArgs a)
@@ -1131,7 +1133,9 @@ constexpr long long kPairs = 256;           // a workgroup holds a CU
 // scans in front of the block numbers, and a quarter of the groups in a row.
 // Through a window (WINDOW) the block numbers wait for the length, one round trip more: one sequence through 512 + 4
 // tokens (40 heads over 8, E4M3) in parts 6.2 us and the merge 3, 13 through 1021 + 13 (32 over 8 of 64 dims, E5M2) 7.6
-// and 3; round trips bound both (1.1 and 13 MB).
+// and 3; round trips bound both (1.1 and 13 MB).  A pass of the fused step / of decode alone / of write and decode apart:
+// these two 9.6 / 9.1 / 11.7 us and 12.0 / 10.8 / 15.1; in one launch, one sequence through 256 + 4 7.6 / 7.5 / 10.0, through
+// 128 + 4 over an fp16 cache 6.6 / 6.5 / 8.5.
 template <int HEAD_DIM, int KV, bool BIG, bool APPEND, bool PARTS, bool WINDOW = false>
 __global__ void __launch_bounds__(64 * (PARTS ? kPartWaves : kPairWaves), PARTS ? 1 : 2)
 pair_decode_kernel(const FlatArgs a)

@@ -171,9 +171,12 @@ __device__ __forceinline__ float wide_logits_window(floatx16& z, int j, floatx4 
 // WINDOW: a workgroup streams its rows' view of the sequence (window.hpp) from the first row's window on, and
 // tokens, blocks and lengths are that view's.  A column's window begins up to a workgroup's rows behind the
 // stream's start: the stages in front of the last one's window go group by group, like those at the stream's end.
-// 4 x 2048 rows through 4096 + 4 tokens (40 heads over 8, E4M3): 735 us, 936 TFLOP/s, bound as without a window; 5 fresh
-// prompts of 100 to 1777 rows through 500 + 7 (32 over 8 of 64 dims, fp16): 44 us, of which the workgroups' starts and
-// ends are a third.
+// 4 x 2048 rows through 4096 + 4 tokens (40 heads over 8, E4M3): 735 us, 936 TFLOP/s, bound as without a window; 5
+// fresh prompts of 100 to 1777 rows through 500 + 7 (32 over 8 of 64 dims, fp16): 44 us, of which the workgroups'
+// starts and ends are a third.  In pools beyond 2 GiB (BIG), whose bases are 64 bits wide, the one-byte forms of
+// 128 dims but one keep 2 to 4 registers in memory: pool just below / just above 2 GiB, that first launch 731 /
+// 732 us and 771 / 795 with E5M2, 8 x 500 rows through 2048 + 4 232 / 233 and 250 / 265 (without a window, which
+// spills nothing, 730 / 731 and 764 / 771).
 template <int HEAD_DIM, int KV, int TILES, bool BIG, bool WINDOW = false>
 __global__ void __launch_bounds__(64 * kPrefillWaves, 2)
 prefill_chunk_kernel(const PrefillArgs a)

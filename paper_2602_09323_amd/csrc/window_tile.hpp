@@ -15,12 +15,13 @@ inline int window_tile_sets(const coopt_shape* sh) { return sh->head_dim == 128 
 
 constexpr int kWindowTileGroups = 64;       // two-block groups per wavefront: two registers of block numbers
 
-// What a launch takes, in us, by a model of its two sides that was fitted to 250 measurements (dims 128 / 64; 11 % off on
-// average, and what it chooses takes 1.3 % longer than the best choice).  A tile's own time: for every group of a wavefront
-// 0.68 / 0.56 (two sets: 1.12 / 0.74), or what one CU reads of its view (97 GB/s), and the merge.  The chip's: of a SIMD,
-// 3 / 1.7 for a wavefront and 0.39 / 0.22 for its groups (two sets: 3.3 / 2 and 0.64 / 0.36), times the wavefronts that it
-// has, half way to the next whole number; or the views from the L2 (21 TB/s) or the pairs' from HBM.  The longer one
-// counts, and 0.39 of the other.
+// What a launch takes, in us, by a model of its two sides that was fitted to 250 measurements (dims 128 / 64; 11 % off
+// on average, and what it chooses takes 1.7 % longer than the best choice, 22 % at most; it is off most often for fp16,
+// whose views from the L2 it takes for slower than they are: of the rows below 30.8 us where 26.4 was to be had, 33.0
+// where 30.1).  A tile's own time: for every group of a wavefront 0.68 / 0.56 (two sets: 1.12 / 0.74), or what one CU
+// reads of its view (97 GB/s), and the merge.  The chip's: of a SIMD, 3 / 1.7 for a wavefront and 0.39 / 0.22 for its
+// groups (two sets: 3.3 / 2 and 0.64 / 0.36), times the wavefronts that it has, half way to the next whole number; or
+// the views from the L2 (21 TB/s) or the pairs' from HBM.  The longer one counts, and 0.39 of the other.
 inline double tile_us(const coopt_shape* sh, double tiles, int groups, int waves, int sets)
 {
     const bool wide = sh->head_dim == 128, two = sets == 2;
